@@ -253,6 +253,101 @@ int speca_linear(void* hip_stream, int dtype, const void* a, int m, int k, const
  * out: DEVICE [rows][tokens][heads*head_dim], both of type dtype.  Asynchronous on hip_stream. */
 int speca_attention(void* hip_stream, int dtype, const void* qkv, void* out, int rows, int tokens, int heads, int head_dim);
 
+/* ---- attention of packed and cached sequences, callable on its own --------------------------- */
+
+/* Common to the five calls below.  Tensors are DEVICE memory; a token's heads lie one after the other ([heads][head_dim]
+ * without gaps) and tokens are ld elements apart, so q, k and v may be views of one layer's output [tokens][(H + 2 Hkv) head_dim].
+ * Query head h reads key and value head h / (heads / kv_heads); heads must be a multiple of kv_heads.
+ * Sequences of different lengths are laid end to end: sequence s holds tokens starts[s] .. starts[s + 1] - 1 of a buffer of `total`
+ * tokens (starts: DEVICE int32 [n_seqs + 1], rising; a sequence may be empty).  Tokens below starts[0] and from starts[n_seqs] on
+ * are neither read nor written.  Offsets are clamped to 0 .. total, so none reads or writes outside the buffers.
+ * Everything is asynchronous on hip_stream, whose device must be the current one; nothing is allocated, kept or synchronised, so calls may be captured
+ * into a HIP graph.  No tokens (total = 0) is no work.  Errors: message via speca_last_error(NULL).  Results do not depend on
+ * timing: the same inputs give the same bits. */
+
+enum { SPECA_ROPE_ADJACENT = 0, SPECA_ROPE_HALVES = 1 };
+enum { SPECA_ROPE_PER_AXIS = 0, SPECA_ROPE_JOINT = 1 };
+#define SPECA_ROPE_MAX_AXES 4
+/* Rotary positions with several axes (time, height, width).  R = sum of dims features of a head turn in R / 2 pairs; the features
+ * from R on stay.  Pair i is features (2i, 2i + 1) (ADJACENT) or (i, i + R / 2) (HALVES).  The first dims[0] / 2 pairs turn with the
+ * first axis, the next dims[1] / 2 with the second, ...: pair j of axis a by
+ *   position[a] * scale[a] * theta[a]^(-2 j / dims[a])        (PER_AXIS: every axis has its own spectrum)
+ *   position[a] * scale[a] * theta[0]^(-2 i / R)              (JOINT: one spectrum over all pairs, i = pair of the head)
+ * radians, formed in 64 bits, so far positions keep their angle. */
+typedef struct speca_rope {
+  int32_t axes;                        /* 1 .. SPECA_ROPE_MAX_AXES */
+  int32_t dims[SPECA_ROPE_MAX_AXES];   /* features of each axis: even, >= 2 */
+  float theta[SPECA_ROPE_MAX_AXES];    /* > 0 */
+  float scale[SPECA_ROPE_MAX_AXES];    /* 1 = positions as they are; < 1 = positions drawn together */
+  int32_t pairing;                     /* SPECA_ROPE_ADJACENT | SPECA_ROPE_HALVES */
+  int32_t spectrum;                    /* SPECA_ROPE_PER_AXIS | SPECA_ROPE_JOINT */
+} speca_rope;
+/* One of the two tensors of speca_rope_axes. */
+typedef struct speca_rope_io {
+  const void* x;                       /* [tokens][heads][head_dim], tokens ldx elements apart */
+  void* out;                           /* the same, ldo apart; may be x (then ldo = ldx), may not overlap it otherwise */
+  const void* norm;                    /* [head_dim] weight of the RMS norm of every head ahead of the rotation, or NULL: no norm */
+  int64_t ldx, ldo;
+  int32_t heads;
+} speca_rope_io;
+/* q (and k unless NULL): x <- x / sqrt(mean(x^2) + eps) * norm per head, then the rotation; fp32 arithmetic, one rounding.
+ * positions: DEVICE int32 [tokens][axes].  head_dim even, 2 .. 128. */
+int speca_rope_axes(void* hip_stream, int dtype, const speca_rope* rope, const int32_t* positions, int64_t tokens, int head_dim,
+                    float eps, const speca_rope_io* q, const speca_rope_io* k);
+
+/* out = softmax(scale q k^T) v inside every sequence; causal != 0: a token sees itself and the tokens before it.
+ * scale 0 = 1 / sqrt(head_dim).  out: [total][heads][head_dim], tokens ldo apart.  head_dim 16, 32, 64, 72 or 128.  What a token
+ * does not see has no part in its result, whatever it holds (infinities and NaN included). */
+int speca_attention_packed(void* hip_stream, int dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                           void* out, int64_t ldo, const int32_t* starts, int n_seqs, int total, int heads, int kv_heads, int head_dim,
+                           int causal, float scale);
+
+/* Keys and values of past tokens in 8 bits.  A page holds SPECA_KV_PAGE tokens of every key head, all memory is the caller's:
+ *   k        bytes [pages][kv_heads][64 tokens][head_dim]
+ *   v        bytes [pages][kv_heads][head_dim][64 tokens], token 16 m + 4 g + i of the page at place 16 g + 4 m + i (m, g, i < 4):
+ *            what one lane of a matrix instruction reads is then 16 bytes in one piece
+ *   k_scale, v_scale  float [pages][kv_heads]
+ * A byte is e4m3 (OCP: largest 448, 0x7F and 0xFF are NaN) and stands for its value x the scale of its page and head, a power of
+ * two 2^e with -100 <= e <= 119, the smallest whose 448-fold reaches every finite value that was stored in the page (or larger, where
+ * larger tokens have been overwritten).  With powers of two, bytes times scale are exact in bf16, and a page that grows keeps its tokens'
+ * values when a larger token takes the scale up, unless they become subnormal (below scale / 64; then rounded once more).
+ * k and v must be 16-byte aligned.  head_dim 16, 32, 64, 72 or 128. */
+#define SPECA_KV_PAGE 64
+typedef struct speca_kv_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int32_t pages, kv_heads, head_dim;
+} speca_kv_cache;
+/* Page number of token 64 j of sequence s: page[s * ld + j], DEVICE int32.  Tokens from 64 ld on, and those whose page number lies outside
+ * 0 .. pages - 1, are not held: they are not stored, load as zeros and are not attended to. */
+typedef struct speca_kv_table {
+  const int32_t* page;
+  int32_t ld;
+} speca_kv_table;
+
+/* Tokens of the packed k and v ([total][kv_heads][head_dim] of type dtype) become tokens past[s], past[s] + 1, ... of sequence s (past: DEVICE
+ * int32 [n_seqs], >= 0).  Rounding to nearest, ties to even; infinities saturate, NaN stays.  Tokens of a page below past[s] are kept, what lay from the last new token
+ * on in its page is cleared.  Two sequences of one call must not write the same page. */
+int speca_kv_store(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* past,
+                   const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total);
+/* The other way round: tokens first[s], first[s] + 1, ... of sequence s, as the values they stand for, into packed k and v. */
+int speca_kv_load(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* first,
+                  void* k, int64_t ldk, void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total);
+
+/* Attention of the new tokens q ([total][heads][head_dim], bf16) over the first lens[s] tokens of their sequence in the cache
+ * (lens: DEVICE int32 [n_seqs]; the new tokens' own keys are among them if they were stored).  causal != 0: of n new tokens the i-th sees tokens 0 .. lens[s] - n + i.
+ * A token that sees nothing (lens[s] = 0, or causal with more new tokens than held) gives 0.  max_len: no sequence is longer (tokens from there
+ * on are not attended to); it sets how the work is split, as n_seqs and total do.  out: bf16, tokens ldo apart.
+ * dtype: SPECA_BF16 (SPECA_F32 is SPECA_EUNSUPPORTED).  workspace: DEVICE, 16-byte aligned, of at least
+ * speca_attention_cached_workspace bytes, in use until the call's work has ended; calls that may overlap need one each. */
+int speca_attention_cached(void* hip_stream, int dtype, const void* q, int64_t ldq, void* out, int64_t ldo, const int32_t* starts, int n_seqs,
+                           int total, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* lens, int max_len, int heads,
+                           int causal, float scale, void* workspace, int64_t workspace_bytes);
+/* Bytes of workspace for these sizes (0: none, the pointer may be NULL); -1 if a size is not valid.  Host only. */
+int64_t speca_attention_cached_workspace(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim);
+
 /* ---- measurement ----------------------------------------------------------------------------- */
 
 /* Kernel classes of the per-class timing below. */

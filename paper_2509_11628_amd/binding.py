@@ -19,9 +19,13 @@ COEF_TAYLOR, COEF_NEWTON, COEF_ADAMS_BASHFORTH = 0, 1, 2
 SOLVER_DDIM, SOLVER_FLOW, SOLVER_DDPM = 0, 1, 2
 CACHE_DIFFERENCES, CACHE_RING = 0, 1
 KIND_FULL, KIND_SPEC, KIND_REJECT = 0, 1, 2
+ROPE_ADJACENT, ROPE_HALVES = 0, 1
+ROPE_PER_AXIS, ROPE_JOINT = 0, 1
 METRIC_L2, METRIC_L1, METRIC_LINF, METRIC_COSINE = 0, 1, 2, 3
 MAX_ORDER = 4
 MAX_LAUNCH_ROWS = 64
+ROPE_MAX_AXES = 4
+KV_PAGE = 64
 
 
 class SpecaError(RuntimeError):
@@ -68,6 +72,24 @@ class Profile(C.Structure):
     _fields_ = [("launches", C.c_int64 * 6), ("ms", C.c_double * 6), ("flops", C.c_double * 6), ("bytes", C.c_double * 6)]
 
 
+class Rope(C.Structure):
+    _fields_ = [("axes", C.c_int32), ("dims", C.c_int32 * ROPE_MAX_AXES), ("theta", C.c_float * ROPE_MAX_AXES),
+                ("scale", C.c_float * ROPE_MAX_AXES), ("pairing", C.c_int32), ("spectrum", C.c_int32)]
+
+
+class RopeIO(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("norm", C.c_void_p), ("ldx", C.c_int64), ("ldo", C.c_int64), ("heads", C.c_int32)]
+
+
+class KVCacheDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class KVTable(C.Structure):
+    _fields_ = [("page", C.c_void_p), ("ld", C.c_int32)]
+
+
 PROF_CLASSES = ["gemm", "attention", "forecast", "verify", "refresh", "other"]
 
 _lib = None
@@ -99,6 +121,12 @@ def load_library() -> C.CDLL:
         "speca_sample": [vp, vp, C.c_int, C.POINTER(Cond), C.POINTER(Solver), f32p, C.POINTER(Trace)],
         "speca_linear": [vp, C.c_int, vp, C.c_int, C.c_int, vp, C.c_int, vp, C.c_int, vp],
         "speca_attention": [vp, C.c_int, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int],
+        "speca_rope_axes": [vp, C.c_int, C.POINTER(Rope), vp, C.c_int64, C.c_int, C.c_float, C.POINTER(RopeIO), C.POINTER(RopeIO)],
+        "speca_attention_packed": [vp, C.c_int] + [vp, C.c_int64] * 4 + [vp] + [C.c_int] * 6 + [C.c_float],
+        "speca_kv_store": [vp, C.c_int, C.POINTER(KVCacheDesc), C.POINTER(KVTable), vp, vp, C.c_int64, vp, C.c_int64, vp, C.c_int, C.c_int],
+        "speca_kv_load": [vp, C.c_int, C.POINTER(KVCacheDesc), C.POINTER(KVTable), vp, vp, C.c_int64, vp, C.c_int64, vp, C.c_int, C.c_int],
+        "speca_attention_cached": [vp, C.c_int, vp, C.c_int64, vp, C.c_int64, vp, C.c_int, C.c_int, C.POINTER(KVCacheDesc), C.POINTER(KVTable),
+                                   vp, C.c_int, C.c_int, C.c_int, C.c_float, vp, C.c_int64],
         "speca_set_lanes": [vp, C.c_int, C.c_int],
         "speca_profile_begin": [vp],
         "speca_profile_end": [vp, C.POINTER(Profile)],
@@ -119,13 +147,16 @@ def load_library() -> C.CDLL:
         fn.restype = C.c_int
     lib.speca_last_error.argtypes = [vp]
     lib.speca_last_error.restype = C.c_char_p
+    lib.speca_attention_cached_workspace.argtypes = [C.c_int] * 6
+    lib.speca_attention_cached_workspace.restype = C.c_int64
     _lib = lib
     return lib
 
 
 EXPORTED = ["speca_create", "speca_destroy", "speca_last_error", "speca_init_cache", "speca_refresh",
             "speca_full_step", "speca_forecast", "speca_verify", "speca_verify_static", "speca_spec_step", "speca_sample",
-            "speca_linear", "speca_attention", "speca_set_lanes", "speca_profile_begin", "speca_profile_end",
+            "speca_linear", "speca_attention", "speca_rope_axes", "speca_attention_packed", "speca_kv_store", "speca_kv_load",
+            "speca_attention_cached", "speca_attention_cached_workspace", "speca_set_lanes", "speca_profile_begin", "speca_profile_end",
             "speca_tau_geometric", "speca_tau_linear", "speca_coefficients", "speca_divisors",
             "speca_ring_weights", "speca_sched_create", "speca_sched_destroy", "speca_sched_plan", "speca_sched_commit",
             "speca_sched_refs"]
@@ -224,6 +255,182 @@ def attention(qkv, heads: int, out=None):
                                C.c_void_p(out.data_ptr()), rows, T, heads, D // heads)
     if code != OK:
         raise SpecaError(code, lib.speca_last_error(None).decode())
+    return out
+
+
+# ---- attention of packed and cached sequences ------------------------------------------------
+
+
+def _heads(name, x, like=None):
+    """A tensor [tokens, heads, head_dim] whose heads lie one after the other: its distance between tokens."""
+    import torch
+    if x.dim() != 3 or x.stride(2) != 1 and x.shape[2] > 1 or x.stride(1) != x.shape[2] and x.shape[1] > 1:
+        raise ValueError(f"{name}: [tokens, heads, head_dim] with the heads of a token in one piece is wanted, got {tuple(x.shape)} with strides {x.stride()}")
+    if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"{name}: a bf16 or fp32 device tensor is wanted, got {x.dtype} on {x.device}")
+    if like is not None and (x.dtype != like.dtype or x.device != like.device):
+        raise ValueError(f"{name}: {x.dtype} on {x.device}, the others are {like.dtype} on {like.device}")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+
+
+def _ints(name, x, shape, like):
+    """A contiguous int32 tensor on the device of `like`; None in `shape`: any size."""
+    import torch
+    if x.dtype != torch.int32 or x.device != like.device or not x.is_contiguous() or x.dim() != len(shape) or any(
+            n is not None and n != m for n, m in zip(shape, x.shape)):
+        raise ValueError(f"{name}: contiguous int32 {shape} on {like.device} is wanted, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+def _stand_alone(like, name, *args):
+    """Call an entry point without a context on the current stream of `like`'s device."""
+    import torch
+    lib = load_library()
+    if like.device.index != torch.cuda.current_device():
+        with torch.cuda.device(like.device):
+            return _stand_alone(like, name, *args)
+    code = getattr(lib, name)(torch.cuda.current_stream().cuda_stream, BF16 if like.dtype == torch.bfloat16 else F32, *args)
+    if code != OK:
+        raise SpecaError(code, lib.speca_last_error(None).decode())
+
+
+def make_rope(dims, theta=10000.0, scale=1.0, pairing=ROPE_ADJACENT, spectrum=ROPE_PER_AXIS) -> Rope:
+    """dims: features that turn with each axis; theta, scale: one number or one per axis."""
+    n = len(dims)
+    if not 1 <= n <= ROPE_MAX_AXES:
+        raise ValueError(f"1 to {ROPE_MAX_AXES} axes, got {n}")
+    per = [list(v) if isinstance(v, (list, tuple)) else [v] * n for v in (theta, scale)]
+    if any(len(v) != n for v in per):
+        raise ValueError("theta and scale: one number, or one per axis")
+    pad = [0] * (ROPE_MAX_AXES - n)
+    return Rope(n, (C.c_int32 * ROPE_MAX_AXES)(*dims, *pad), (C.c_float * ROPE_MAX_AXES)(*per[0], *pad), (C.c_float * ROPE_MAX_AXES)(*per[1], *pad),
+                pairing, spectrum)
+
+
+def rope_axes(rope: Rope, positions, q, k=None, q_norm=None, k_norm=None, eps: float = 1e-6, out=None):
+    """speca_rope_axes: q [tokens, heads, head_dim], k [tokens, kv_heads, head_dim] (views of one layer's output, for instance), positions
+    int32 [tokens, axes].  -> (q, k) turned, into `out` (a pair, which may be q and k themselves) or new tensors; without k: q alone."""
+    import torch
+    sides, made = [], []
+    for i, (name, x, norm) in enumerate((("q", q, q_norm), ("k", k, k_norm))):
+        if x is None:
+            continue
+        ldx = _heads(name, x, q)
+        if x.shape[0] != q.shape[0] or x.shape[2] != q.shape[2]:
+            raise ValueError(f"{name}: {tuple(x.shape)}, q is {tuple(q.shape)}")
+        if norm is not None and (norm.dtype != q.dtype or norm.device != q.device or tuple(norm.shape) != (q.shape[2],) or not norm.is_contiguous()):
+            raise ValueError(f"{name}_norm: a weight [{q.shape[2]}] of the same type is wanted")
+        o = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out if k is None and not isinstance(out, (tuple, list)) else out[i]
+        ldo = _heads(name + " out", o, q)
+        if o.shape != x.shape:
+            raise ValueError(f"{name} out: {tuple(o.shape)}, {name} is {tuple(x.shape)}")
+        made.append(o)
+        sides.append(RopeIO(x.data_ptr(), o.data_ptr(), None if norm is None else norm.data_ptr(), ldx, ldo, x.shape[1]))
+    if q.shape[0]:
+        _stand_alone(q, "speca_rope_axes", rope, _ints("positions", positions, (q.shape[0], rope.axes), q), q.shape[0], q.shape[2], eps, sides[0],
+                     sides[1] if len(sides) > 1 else None)
+    return tuple(made) if len(made) > 1 else made[0]
+
+
+def attention_packed(q, k, v, starts, causal: bool = False, scale: float = 0.0, out=None):
+    """speca_attention_packed: q [total, heads, head_dim], k and v [total, kv_heads, head_dim], starts int32 [n_seqs + 1].
+    -> [total, heads, head_dim]; tokens outside the sequences are left as they are in `out` (in a new tensor: undefined)."""
+    import torch
+    ldq, ldk, ldv = _heads("q", q), _heads("k", k, q), _heads("v", v, q)
+    if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ldo = _heads("out", out, q)
+    if out.shape != q.shape:
+        raise ValueError(f"out: {tuple(out.shape)}, q is {tuple(q.shape)}")
+    at = _ints("starts", starts, (None,), q)
+    if q.shape[0]:
+        _stand_alone(q, "speca_attention_packed", q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, out.data_ptr(), ldo, at, len(starts) - 1,
+                     q.shape[0], q.shape[1], k.shape[1], q.shape[2], int(causal), scale)
+    return out
+
+
+class KVCache:
+    """Pages of keys and values in 8 bits, owned by the caller: k uint8 [pages, kv_heads, 64, head_dim], v uint8 [pages, kv_heads,
+    head_dim, 64], k_scale and v_scale fp32 [pages, kv_heads] (include/speca.h describes what they hold)."""
+
+    def __init__(self, k, v, k_scale, v_scale):
+        import torch
+        p, h, t, hd = k.shape
+        if t != KV_PAGE or tuple(v.shape) != (p, h, hd, t) or tuple(k_scale.shape) != (p, h) or tuple(v_scale.shape) != (p, h):
+            raise ValueError(f"pages {tuple(k.shape)} and {tuple(v.shape)} with scales {tuple(k_scale.shape)} and {tuple(v_scale.shape)} do not fit")
+        if k.dtype != torch.uint8 or v.dtype != torch.uint8 or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+            raise ValueError("pages are uint8, their scales fp32")
+        if not all(x.is_cuda and x.is_contiguous() and x.device == k.device for x in (k, v, k_scale, v_scale)):
+            raise ValueError("pages and scales are contiguous tensors on one device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), p, h, hd)
+
+    @classmethod
+    def empty(cls, pages: int, kv_heads: int, head_dim: int, device="cuda"):
+        import torch
+        return cls(torch.zeros((pages, kv_heads, KV_PAGE, head_dim), dtype=torch.uint8, device=device),
+                   torch.zeros((pages, kv_heads, head_dim, KV_PAGE), dtype=torch.uint8, device=device),
+                   torch.ones((pages, kv_heads), device=device), torch.ones((pages, kv_heads), device=device))
+
+
+def _cached(cache, x, table, first, starts, first_name):
+    """What the three calls on a cache check alike: the table and the two lists of their sequences."""
+    n = len(starts) - 1
+    if x.device != cache.k.device:
+        raise ValueError(f"tokens on {x.device}, the cache is on {cache.k.device}")
+    if x.shape[2] != cache.k.shape[3]:
+        raise ValueError(f"heads of {x.shape[2]}, the cache's have {cache.k.shape[3]}")
+    return KVTable(_ints("table", table, (n, None), x), table.shape[1]), _ints(first_name, first, (n,), x), _ints("starts", starts, (None,), x), n
+
+
+def kv_store(cache: KVCache, table, past, k, v, starts):
+    """speca_kv_store: k and v [total, kv_heads, head_dim] become tokens past[s], past[s] + 1, ... of sequence s (rows starts[s] ..
+    starts[s + 1]); table int32 [n_seqs, pages of a sequence], past int32 [n_seqs]."""
+    ldk, ldv = _heads("k", k), _heads("v", v, k)
+    if k.shape != v.shape or k.shape[1] != cache.k.shape[1]:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit {cache.k.shape[1]} key heads")
+    t, at, cu, n = _cached(cache, k, table, past, starts, "past")
+    if k.shape[0]:
+        _stand_alone(k, "speca_kv_store", cache.desc, t, at, k.data_ptr(), ldk, v.data_ptr(), ldv, cu, n, k.shape[0])
+
+
+def kv_load(cache: KVCache, table, first, starts, total: int, dtype, out=None):
+    """speca_kv_load: tokens first[s], first[s] + 1, ... of every sequence -> (k, v) [total, kv_heads, head_dim]; rows outside the
+    sequences are left as they are in `out` (a pair; in new tensors: undefined)."""
+    import torch
+    if out is None:
+        out = tuple(torch.empty((total, cache.k.shape[1], cache.k.shape[3]), dtype=dtype, device=cache.k.device) for _ in range(2))
+    k, v = out
+    ldk, ldv = _heads("k", k), _heads("v", v, k)
+    if k.shape != v.shape or k.shape[1] != cache.k.shape[1] or k.shape[0] != total or k.dtype != dtype:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit {total} tokens of {cache.k.shape[1]} key heads in {dtype}")
+    t, at, cu, n = _cached(cache, k, table, first, starts, "first")
+    if total:
+        _stand_alone(k, "speca_kv_load", cache.desc, t, at, k.data_ptr(), ldk, v.data_ptr(), ldv, cu, n, total)
+    return k, v
+
+
+def attention_cached(q, starts, cache: KVCache, table, lens, causal: bool = True, scale: float = 0.0, max_len: Optional[int] = None, out=None):
+    """speca_attention_cached: q bf16 [total, heads, head_dim] over the first lens[s] tokens of their sequence in the cache; max_len: no
+    sequence is longer (default: what the table has room for).  -> [total, heads, head_dim]."""
+    import torch
+    ldq = _heads("q", q)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ldo = _heads("out", out, q)
+    if out.shape != q.shape:
+        raise ValueError(f"out: {tuple(out.shape)}, q is {tuple(q.shape)}")
+    t, at, cu, n = _cached(cache, q, table, lens, starts, "lens")
+    total, heads, hd = q.shape
+    if not total:
+        return out
+    longest = table.shape[1] * KV_PAGE if max_len is None else max_len
+    size = load_library().speca_attention_cached_workspace(n, total, longest, heads, cache.k.shape[1], hd)
+    room = torch.empty(size, dtype=torch.uint8, device=q.device) if size > 0 else None
+    _stand_alone(q, "speca_attention_cached", q.data_ptr(), ldq, out.data_ptr(), ldo, cu, n, total, cache.desc, t, at, longest, heads, int(causal), scale,
+                 None if room is None else room.data_ptr(), max(size, 0))
     return out
 
 

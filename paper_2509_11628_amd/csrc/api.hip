@@ -9,6 +9,7 @@
 #include "gemm.h"
 #include "kernels.h"
 #include "model.h"
+#include "operators.h"
 
 using namespace speca;
 
@@ -469,6 +470,18 @@ Error sample_impl(speca_ctx* ctx, float* latents, int batch, const speca_cond* c
                   speca_trace* trace);
 }
 
+// An entry point without a context: its message goes where speca_last_error(NULL) finds it, and nothing is thrown.
+template <typename F>
+static int stand_alone(F&& call) {
+  try {
+    const Error r = call();
+    if (r.code != SPECA_OK) g_create_error = r.msg;
+    return r.code;
+  } catch (...) {
+    return SPECA_ENOMEM;             // of a message
+  }
+}
+
 extern "C" {
 
 int speca_create(speca_ctx** out, const speca_model_desc* desc, const speca_weights* w, void* hip_stream) {
@@ -552,6 +565,53 @@ int speca_attention(void* hip_stream, int dtype, const void* qkv, void* out, int
   Error r = launch_attention(dtype, qkv, out, static_cast<int64_t>(heads) * head_dim, rows, tokens, heads, head_dim, static_cast<hipStream_t>(hip_stream));
   if (r.code != SPECA_OK) g_create_error = r.msg;
   return r.code;
+}
+
+int speca_rope_axes(void* hip_stream, int dtype, const speca_rope* rope, const int32_t* positions, int64_t tokens, int head_dim, float eps,
+                    const speca_rope_io* q, const speca_rope_io* k) {
+  return stand_alone([&]() -> Error {
+    if (!rope || !q) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: rope and q must not be NULL");
+    return launch_rope_axes(dtype, *rope, positions, tokens, head_dim, eps, *q, k, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int speca_attention_packed(void* hip_stream, int dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
+                           void* out, int64_t ldo, const int32_t* starts, int n_seqs, int total, int heads, int kv_heads, int head_dim,
+                           int causal, float scale) {
+  return stand_alone([&] {
+    return launch_attention_packed(dtype, {q, k, v, out, ldq, ldk, ldv, ldo, {starts, n_seqs, total}, heads, kv_heads, head_dim, causal != 0, scale},
+                                   static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int speca_kv_store(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* past, const void* k,
+                   int64_t ldk, const void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total) {
+  return stand_alone([&]() -> Error {
+    if (!cache || !table) SPECA_FAIL(SPECA_EINVAL, "speca_kv_store: cache and table must not be NULL");
+    return launch_kv_store(dtype, *cache, *table, past, k, ldk, v, ldv, {starts, n_seqs, total}, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int speca_kv_load(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* first, void* k,
+                  int64_t ldk, void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total) {
+  return stand_alone([&]() -> Error {
+    if (!cache || !table) SPECA_FAIL(SPECA_EINVAL, "speca_kv_load: cache and table must not be NULL");
+    return launch_kv_load(dtype, *cache, *table, first, k, ldk, v, ldv, {starts, n_seqs, total}, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int speca_attention_cached(void* hip_stream, int dtype, const void* q, int64_t ldq, void* out, int64_t ldo, const int32_t* starts, int n_seqs,
+                           int total, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* lens, int max_len, int heads,
+                           int causal, float scale, void* workspace, int64_t workspace_bytes) {
+  return stand_alone([&]() -> Error {
+    if (!cache || !table) SPECA_FAIL(SPECA_EINVAL, "speca_attention_cached: cache and table must not be NULL");
+    return launch_attention_cached(dtype, *cache, *table, {q, out, ldq, ldo, {starts, n_seqs, total}, lens, max_len, heads, causal != 0, scale}, workspace,
+                                   workspace_bytes, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int64_t speca_attention_cached_workspace(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
+  return attention_cached_workspace(n_seqs, total, max_len, heads, kv_heads, head_dim);
 }
 
 int speca_profile_begin(speca_ctx* ctx) {

@@ -1,0 +1,500 @@
+// Attention of new tokens over keys and values in 8-bit pages.
+//
+// One block = 16 NQ rows of one (sequence, key head); a row is one query head of one new token, so the heads that share a key head share its
+// reads.  Four waves take the pages w, w + 4, ... of the block's range with an online softmax of their own and merge at the end; where rows are
+// few, the range of keys is split over blocks as well, whose sums a second launch joins.
+//   S^T[key][row] = K q^T,  O^T[d][row] += V^T P^T   (bf16 16x16x32 instructions, keys and values widened from e4m3 under their page's
+// scale, exactly: the scale is a power of two)
+// Nothing goes through LDS on its way: a page's layout is the operands' one.  Lane (l, g) of an operand wants 8 of 32 columns of key 16 m + l; it
+// takes 16 bytes at 16 g, which serve two instructions (the order of the columns is a dummy, q follows it).  Of value dimension d it wants the
+// keys in the order in which S^T holds them (4 g .. 4 g + 3 of every 16), which is how the page stores them: 16 bytes per dimension.
+#include <algorithm>
+#include <cmath>
+
+#include "gemm.h"
+#include "operators.h"
+
+namespace speca {
+
+namespace {
+
+constexpr int PAGE = SPECA_KV_PAGE;
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_at8 __attribute__((ext_vector_type(4), aligned(8)));       // head size 72: rows of 72 bytes
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+union Frag {
+  uint32_t u[4];
+  bf16x8 v;
+};
+
+__device__ inline uint32_t cvt_pk_bf16(float a, float b) {
+  const bf16x2 r = __builtin_convertvector(floatx2{a, b}, bf16x2);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+// four e4m3 bytes x a power of two -> four bf16
+__device__ inline void widen(uint32_t b, float scale, uint32_t* out) {
+  const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+  out[0] = *reinterpret_cast<const uint32_t*>(&lo);
+  out[1] = *reinterpret_cast<const uint32_t*>(&hi);
+}
+// maximum over the lanes l % 16 + {0, 16, 32, 48}, which hold one row
+__device__ __forceinline__ float max_of_groups(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float sum_of_groups(float x) {
+  x += __shfl_xor(x, 16, 64);
+  return x + __shfl_xor(x, 32, 64);
+}
+
+struct Args {
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;
+  const uint16_t* q;
+  uint16_t* out;
+  int64_t ldq, ldo;
+  Packed seqs;
+  const int32_t *lens, *table;
+  float *part, *stats;              // of splits: O [block][16 NQ][HD], then maximum and sum [block][2][16 NQ]
+  int32_t table_ld, pages, kv_heads, group;
+  int32_t max_len, splits, split_pages;
+  int32_t causal, wide;             // wide: queries at whole 16 bytes, outputs at whole 8
+  float scale_log2e;
+};
+
+template <int HD, int NQ>
+__global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(const Args g) {
+  constexpr int FULL = HD / 64, REM = HD % 64;
+  constexpr int KS = 2 * FULL + (REM ? 1 : 0);     // steps of 32 columns
+  constexpr int DT = (HD + 15) / 16;
+  constexpr int ROWS = 16 * NQ;
+  static_assert(REM <= 32 && REM % 8 == 0, "head_dim");
+  __shared__ __align__(16) floatx4 merge[4][DT * NQ][64];
+  __shared__ float stat_m[4][ROWS], stat_l[4][ROWS], stat_seen[4][ROWS];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, g4 = lane >> 4;
+  const int split = blockIdx.x % g.splits, rest = blockIdx.x / g.splits, head = rest % g.kv_heads, tile = rest / g.kv_heads;
+  const int seq = packed_find(g.seqs, tile, g.group, ROWS, 0);
+  int start, n;
+  packed_rows(g.seqs, seq, &start, &n);
+  const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS;
+  const int64_t rows = static_cast<int64_t>(n) * g.group;
+  if (r0 < 0 || r0 >= rows) return;
+  int len = g.lens[seq];
+  len = len < 0 ? 0 : min(len, g.max_len);
+
+  // rows 16 i + l16: token, head, number of keys that it sees
+  int tok[NQ], sub[NQ], lim[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int64_t r = r0 + i * 16 + l16 < rows ? r0 + i * 16 + l16 : rows - 1;
+    tok[i] = static_cast<int>(r / g.group);
+    sub[i] = static_cast<int>(r - static_cast<int64_t>(tok[i]) * g.group);
+    lim[i] = g.causal ? max(0, len - n + tok[i] + 1) : len;
+  }
+  const int last_tok = static_cast<int>((min(r0 + ROWS, rows) - 1) / g.group), first_tok = static_cast<int>(r0 / g.group);
+  const int most = g.causal ? max(0, len - n + last_tok + 1) : len, least = g.causal ? max(0, len - n + first_tok + 1) : len;
+  const int begin = split * g.split_pages, end = min(begin + g.split_pages, (most + PAGE - 1) / PAGE);
+
+  bf16x8 qf[KS][NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const uint16_t* qp = g.q + (static_cast<int64_t>(start) + tok[i]) * g.ldq + (static_cast<int64_t>(head) * g.group + sub[i]) * HD;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = s < 2 * FULL ? (s / 2) * 64 + g4 * 16 + (s % 2) * 8 : 64 * FULL + g4 * 8;
+      Frag f;
+      f.u[0] = f.u[1] = f.u[2] = f.u[3] = 0;
+      if (d < HD) {
+        if (g.wide) {
+          const uint4 w = *reinterpret_cast<const uint4*>(qp + d);
+          f.u[0] = w.x; f.u[1] = w.y; f.u[2] = w.z; f.u[3] = w.w;
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f.u[j] = qp[d + 2 * j] | static_cast<uint32_t>(qp[d + 2 * j + 1]) << 16;
+        }
+      }
+      qf[s][i] = f.v;
+    }
+  }
+
+  floatx4 o[DT][NQ];
+  float mref[NQ], lrun[NQ];
+  bool seen[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    mref[i] = -INFINITY;
+    lrun[i] = 0.0f;
+    seen[i] = false;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) o[dt][i] = floatx4{};
+  }
+
+  const int32_t* table = g.table + static_cast<int64_t>(seq) * g.table_ld;
+  u32x4 kr[4][FULL ? FULL : 1], vr[DT];
+  u32x2 kx[4];
+  float ks = 0.0f, vs = 0.0f;
+  auto load_k = [&](int page) {
+    const int64_t unit = static_cast<int64_t>(page) * g.kv_heads + head;
+    const uint8_t* p = g.k + unit * (PAGE * HD) + l16 * HD;
+    ks = g.k_scale[unit];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+#pragma unroll
+      for (int j = 0; j < FULL; ++j) kr[m][j] = *reinterpret_cast<const u32x4_at8*>(p + m * 16 * HD + j * 64 + g4 * 16);
+      if constexpr (REM > 0) {
+        kx[m] = u32x2{0, 0};
+        if (g4 * 8 < REM) kx[m] = *reinterpret_cast<const u32x2*>(p + m * 16 * HD + FULL * 64 + g4 * 8);
+      }
+    }
+  };
+  auto load_v = [&](int page) {
+    const int64_t unit = static_cast<int64_t>(page) * g.kv_heads + head;
+    const uint8_t* p = g.v + unit * (PAGE * HD) + g4 * 16;
+    vs = g.v_scale[unit];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      const int d = dt * 16 + l16;
+      vr[dt] = *reinterpret_cast<const u32x4*>(p + (d < HD ? d : HD - 1) * PAGE);        // beyond the head: any, never stored
+    }
+  };
+  // number of page j of the sequence, or -1: not held
+  auto page_of = [&](int j) {
+    const int p = j < g.table_ld ? table[j] : -1;
+    return __builtin_amdgcn_readfirstlane(p < 0 || p >= g.pages ? -1 : p);
+  };
+
+  for (int j = begin + wave; j < end; j += 4) {
+    const int page = page_of(j);
+    if (page < 0) continue;
+    load_k(page);
+    load_v(page);
+    floatx4 s[4][NQ];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+#pragma unroll
+      for (int t = 0; t < KS; ++t) {
+        Frag f;
+        if (t < 2 * FULL) {
+          widen(kr[m][t / 2][2 * (t % 2)], ks, f.u);
+          widen(kr[m][t / 2][2 * (t % 2) + 1], ks, f.u + 2);
+        } else {
+          widen(kx[m][0], ks, f.u);
+          widen(kx[m][1], ks, f.u + 2);
+        }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) s[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[t][i], t ? s[m][i] : floatx4{}, 0, 0, 0);
+      }
+    }
+    const bool edge = (j + 1) * PAGE > least;
+    bool odd = false;                              // the page holds a NaN that some row does not see
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (j * PAGE + 16 * m + 4 * g4 + e >= lim[i]) s[m][i][e] = -INFINITY;
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {                // bytes past the last token: whatever they are, 0 now
+        const int c = len - (j * PAGE + 16 * m + 4 * g4);
+        const uint32_t keep = c >= 4 ? ~0u : c <= 0 ? 0u : (1u << (8 * c)) - 1u;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          vr[dt][m] &= keep;
+          odd |= (((vr[dt][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+        }
+      }
+      odd = __any(odd);
+    }
+    bool moved = false;
+    float corr[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[m][i][e]);
+      const float mnew = fmaxf(mref[i], max_of_groups(top));
+      const float moff = mnew == -INFINITY ? 0.0f : mnew * g.scale_log2e;          // no finite score yet: weights 0
+      corr[i] = fast_exp2(mref[i] * g.scale_log2e - moff);
+      moved |= mnew != mref[i];
+      mref[i] = mnew;
+      seen[i] |= j * PAGE < lim[i];
+      float sum = 0.0f;
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float p = fast_exp2(fmaf(s[m][i][e], g.scale_log2e, -moff));
+          s[m][i][e] = p;
+          sum += p;
+        }
+      lrun[i] = lrun[i] * corr[i] + sum;
+    }
+    if (__any(moved)) {
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt][i] *= corr[i];
+    }
+    if (odd) {
+      // A NaN counts for the rows that see it and must not meet the probability 0 of the others: it is taken out of the page, and a product of
+      // the places of NaN with the places that a row sees says where it belongs.
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        floatx4 hit[NQ];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Frag a;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t w = vr[dt][2 * u + h], nan = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+            a.u[2 * h] = (nan & 0x80u ? 0x3F80u : 0u) | (nan & 0x8000u ? 0x3F800000u : 0u);
+            a.u[2 * h + 1] = (nan & 0x800000u ? 0x3F80u : 0u) | (nan & 0x80000000u ? 0x3F800000u : 0u);
+            vr[dt][2 * u + h] = w & ~((nan >> 7) * 0xFFu);
+          }
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) {
+            Frag b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const int key = j * PAGE + 16 * (2 * u + e / 2) + 4 * g4 + 2 * (e % 2);
+              b.u[e] = (key < lim[i] ? 0x3F80u : 0u) | (key + 1 < lim[i] ? 0x3F800000u : 0u);
+            }
+            hit[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, u ? hit[i] : floatx4{}, 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NQ; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (hit[i][e] > 0.0f) o[dt][i][e] = __uint_as_float(0x7FC00000u);
+      }
+    }
+    bf16x8 pf[2][NQ];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        Frag f;
+        f.u[0] = cvt_pk_bf16(s[2 * u][i][0], s[2 * u][i][1]);
+        f.u[1] = cvt_pk_bf16(s[2 * u][i][2], s[2 * u][i][3]);
+        f.u[2] = cvt_pk_bf16(s[2 * u + 1][i][0], s[2 * u + 1][i][1]);
+        f.u[3] = cvt_pk_bf16(s[2 * u + 1][i][2], s[2 * u + 1][i][3]);
+        pf[u][i] = f.v;
+      }
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        Frag f;
+        widen(vr[dt][2 * u], vs, f.u);
+        widen(vr[dt][2 * u + 1], vs, f.u + 2);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) o[dt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, pf[u][i], o[dt][i], 0, 0, 0);
+      }
+  }
+
+  // together: everything relative to the largest maximum of the four waves; wave w sums the dimensions of tiles w, w + 4, ...
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const float l = sum_of_groups(lrun[i]);
+    if (g4 == 0) {
+      stat_m[wave][i * 16 + l16] = mref[i];
+      stat_l[wave][i * 16 + l16] = l;
+      stat_seen[wave][i * 16 + l16] = seen[i] ? 1.0f : 0.0f;
+    }
+  }
+  __syncthreads();
+  float top[NQ], total[NQ];
+#pragma unroll
+  for (int i = 0; i < NQ; ++i) {
+    const int r = i * 16 + l16;
+    top[i] = fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
+    const float off = top[i] == -INFINITY ? 0.0f : top[i] * g.scale_log2e;
+    total[i] = 0.0f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total[i] += stat_l[w][r] * fast_exp2(stat_m[w][r] * g.scale_log2e - off);
+    // keys were there, none with a score above -inf: that has no softmax.  No keys: 0
+    if (top[i] == -INFINITY) total[i] = stat_seen[0][r] + stat_seen[1][r] + stat_seen[2][r] + stat_seen[3][r] > 0.0f ? __uint_as_float(0x7FC00000u) : 0.0f;
+    const float f = fast_exp2(mref[i] * g.scale_log2e - off);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) merge[wave][dt * NQ + i][lane] = o[dt][i] * f;
+  }
+  __syncthreads();
+  const int64_t block = blockIdx.x;
+  if (g.splits > 1 && wave == 0 && g4 == 0) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      g.stats[block * 2 * ROWS + i * 16 + l16] = top[i];
+      g.stats[block * 2 * ROWS + ROWS + i * 16 + l16] = total[i];
+    }
+  }
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt) {
+    if (dt % 4 != wave) continue;
+    const int d = dt * 16 + 4 * g4;
+    if (d >= HD) continue;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const floatx4 v = (merge[0][dt * NQ + i][lane] + merge[1][dt * NQ + i][lane]) + (merge[2][dt * NQ + i][lane] + merge[3][dt * NQ + i][lane]);
+      if (g.splits > 1) {
+        *reinterpret_cast<floatx4*>(g.part + (block * ROWS + i * 16 + l16) * HD + d) = v;
+      } else if (r0 + i * 16 + l16 < rows) {
+        uint16_t* op = g.out + (static_cast<int64_t>(start) + tok[i]) * g.ldo + (static_cast<int64_t>(head) * g.group + sub[i]) * HD + d;
+        const float inv = total[i] == 0.0f ? 0.0f : 1.0f / total[i];
+        const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
+        if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
+        else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+      }
+    }
+  }
+}
+
+// Joins the splits of 16 NQ rows, in their order.
+template <int HD, int NQ>
+__global__ __launch_bounds__(256) void attention_cached_join_kernel(const Args g) {
+  constexpr int ROWS = 16 * NQ;
+  const int head = blockIdx.x % g.kv_heads, tile = blockIdx.x / g.kv_heads;
+  const int seq = packed_find(g.seqs, tile, g.group, ROWS, 0);
+  int start, n;
+  packed_rows(g.seqs, seq, &start, &n);
+  const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS;
+  const int64_t rows = static_cast<int64_t>(n) * g.group;
+  if (r0 < 0 || r0 >= rows) return;
+  const int64_t first = static_cast<int64_t>(blockIdx.x) * g.splits;
+  for (int at = threadIdx.x; at < ROWS * (HD / 4); at += 256) {
+    const int r = at / (HD / 4), d = (at - r * (HD / 4)) * 4;
+    if (r0 + r >= rows) break;
+    float top = -INFINITY;
+    for (int s = 0; s < g.splits; ++s) top = fmaxf(top, g.stats[(first + s) * 2 * ROWS + r]);
+    const float off = top == -INFINITY ? 0.0f : top * g.scale_log2e;
+    float total = 0.0f;
+    floatx4 v = {};
+    for (int s = 0; s < g.splits; ++s) {
+      const float m = g.stats[(first + s) * 2 * ROWS + r], l = g.stats[(first + s) * 2 * ROWS + ROWS + r];
+      if (m == -INFINITY && top != -INFINITY) continue;
+      const float f = m == -INFINITY ? 1.0f : fast_exp2(m * g.scale_log2e - off);
+      total += l * f;
+      v += *reinterpret_cast<const floatx4*>(g.part + ((first + s) * ROWS + r) * HD + d) * f;
+    }
+    const int tok = static_cast<int>((r0 + r) / g.group), sub = static_cast<int>(r0 + r - static_cast<int64_t>(tok) * g.group);
+    uint16_t* op = g.out + (static_cast<int64_t>(start) + tok) * g.ldo + (static_cast<int64_t>(head) * g.group + sub) * HD + d;
+    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+    const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
+    if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
+    else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+  }
+}
+
+struct Plan {
+  int nq, splits, split_pages;
+  int64_t tiles, blocks;
+  size_t part_bytes, bytes;
+};
+Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
+  Plan p{};
+  const int group = heads / kv_heads;
+  const int64_t rows = static_cast<int64_t>(total) * group, mean = (rows + n_seqs - 1) / n_seqs;
+  p.nq = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
+  p.tiles = rows / (16 * p.nq) + n_seqs;
+  const int pages = (max_len + PAGE - 1) / PAGE;
+  // as many blocks as give every unit four, each of at least 8 pages
+  const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(p.tiles, n_seqs * ((mean + 16 * p.nq - 1) / (16 * p.nq)))) * kv_heads;
+  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((4 * 256 + busy - 1) / busy, pages / 8)));
+  p.split_pages = std::max(1, (pages + p.splits - 1) / p.splits);
+  p.splits = std::max(1, (pages + p.split_pages - 1) / p.split_pages);
+  p.blocks = p.tiles * kv_heads * p.splits;
+  if (p.splits > 1) {
+    p.part_bytes = static_cast<size_t>(p.blocks) * 16 * p.nq * head_dim * sizeof(float);
+    p.bytes = p.part_bytes + static_cast<size_t>(p.blocks) * 2 * 16 * p.nq * sizeof(float);
+  }
+  return p;
+}
+
+template <int HD, int NQ>
+void launch_nq(const Args& g, const Plan& p, hipStream_t st) {
+  attention_cached_kernel<HD, NQ><<<static_cast<unsigned>(p.blocks), 256, 0, st>>>(g);
+  if (p.splits > 1) attention_cached_join_kernel<HD, NQ><<<static_cast<unsigned>(p.tiles * g.kv_heads), 256, 0, st>>>(g);
+}
+template <int HD>
+void launch_hd(const Args& g, const Plan& p, hipStream_t st) {
+  if (p.nq == 1) launch_nq<HD, 1>(g, p, st);
+  else if (p.nq == 2) launch_nq<HD, 2>(g, p, st);
+  else launch_nq<HD, 4>(g, p, st);
+}
+
+bool sizes_ok(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
+  return n_seqs >= 1 && total >= 0 && max_len >= 0 && max_len <= (1 << 30) && heads >= 1 && heads <= 65536 && kv_heads >= 1 && heads % kv_heads == 0 &&
+         (head_dim == 16 || head_dim == 32 || head_dim == 64 || head_dim == 72 || head_dim == 128);
+}
+
+}  // namespace
+
+int64_t attention_cached_workspace(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
+  if (!sizes_ok(n_seqs, total, max_len, heads, kv_heads, head_dim)) return -1;
+  return total == 0 ? 0 : static_cast<int64_t>(plan_of(n_seqs, total, max_len, heads, kv_heads, head_dim).bytes);
+}
+
+Error launch_attention_cached(int dtype, const speca_kv_cache& c, const speca_kv_table& t, const CachedAttention& a, void* workspace,
+                              int64_t workspace_bytes, hipStream_t st) {
+  const char* who = "speca_attention_cached";
+  if (dtype == SPECA_F32) SPECA_FAIL(SPECA_EUNSUPPORTED, "%s: bf16 only", who);
+  if (dtype != SPECA_BF16) SPECA_FAIL(SPECA_EINVAL, "%s: dtype = %d", who, dtype);
+  SPECA_TRY(check_kv_cache(who, c, t));
+  if (!a.q || !a.out || !a.seqs.cu || !a.lens) SPECA_FAIL(SPECA_EINVAL, "%s: q, out, starts and lens must not be NULL", who);
+  if (a.heads < 1 || a.heads > 65536 || a.heads % c.kv_heads) SPECA_FAIL(SPECA_EINVAL, "%s: %d heads over %d key heads", who, a.heads, c.kv_heads);
+  if (!sizes_ok(a.seqs.n, a.seqs.total, a.max_len, a.heads, c.kv_heads, c.head_dim))
+    SPECA_FAIL(SPECA_EINVAL, "%s: n_seqs = %d, total = %d, max_len = %d", who, a.seqs.n, a.seqs.total, a.max_len);
+  const int64_t w = static_cast<int64_t>(a.heads) * c.head_dim, most = int64_t{1} << 40;
+  if (a.ldq < w || a.ldo < w || a.ldq > most || a.ldo > most)
+    SPECA_FAIL(SPECA_EINVAL, "%s: tokens %lld and %lld elements apart, heads need %lld", who, static_cast<long long>(a.ldq), static_cast<long long>(a.ldo), static_cast<long long>(w));
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a.q), to = reinterpret_cast<uintptr_t>(a.out);
+  if (at % 2 || to % 2 || (reinterpret_cast<uintptr_t>(a.seqs.cu) | reinterpret_cast<uintptr_t>(a.lens)) % 4) SPECA_FAIL(SPECA_EINVAL, "%s: a pointer is not aligned to its type", who);
+  if (!(a.scale >= 0.0f) || !std::isfinite(a.scale)) SPECA_FAIL(SPECA_EINVAL, "%s: scale = %g", who, a.scale);
+  if (a.seqs.total == 0) return ok();
+  const Plan p = plan_of(a.seqs.n, a.seqs.total, a.max_len, a.heads, c.kv_heads, c.head_dim);
+  if (p.blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "%s: %d tokens of %d heads are too many for one call", who, a.seqs.total, a.heads);
+  if (p.bytes && (!workspace || workspace_bytes < static_cast<int64_t>(p.bytes) || reinterpret_cast<uintptr_t>(workspace) % 16))
+    SPECA_FAIL(SPECA_EINVAL, "%s: a workspace of %zu bytes, 16-byte aligned, is needed (given: %lld)", who, p.bytes, static_cast<long long>(workspace ? workspace_bytes : 0));
+  Args g;
+  g.k = static_cast<const uint8_t*>(c.k); g.v = static_cast<const uint8_t*>(c.v);
+  g.k_scale = c.k_scale; g.v_scale = c.v_scale;
+  g.q = static_cast<const uint16_t*>(a.q); g.out = static_cast<uint16_t*>(a.out);
+  g.ldq = a.ldq; g.ldo = a.ldo;
+  g.seqs = a.seqs;
+  g.lens = a.lens; g.table = t.page;
+  g.part = static_cast<float*>(workspace);
+  g.stats = p.bytes ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes) : nullptr;
+  g.table_ld = t.ld; g.pages = c.pages; g.kv_heads = c.kv_heads; g.group = a.heads / c.kv_heads;
+  g.max_len = static_cast<int>(std::min<int64_t>(a.max_len, static_cast<int64_t>(t.ld) * PAGE));
+  g.splits = p.splits; g.split_pages = p.split_pages;
+  g.causal = a.causal;
+  g.wide = at % 16 == 0 && a.ldq % 8 == 0 && to % 8 == 0 && a.ldo % 4 == 0;
+  g.scale_log2e = 1.4426950408889634f * (a.scale == 0.0f ? 1.0f / std::sqrt(static_cast<float>(c.head_dim)) : a.scale);
+  switch (c.head_dim) {
+    case 16: launch_hd<16>(g, p, st); break;
+    case 32: launch_hd<32>(g, p, st); break;
+    case 64: launch_hd<64>(g, p, st); break;
+    case 72: launch_hd<72>(g, p, st); break;
+    default: launch_hd<128>(g, p, st); break;
+  }
+  SPECA_HIP(hipGetLastError());
+  return ok();
+}
+
+}  // namespace speca
