@@ -12,6 +12,7 @@
 #include <cmath>
 
 #include "gemm.h"
+#include "attn_lane.h"
 #include "operators.h"
 
 namespace speca {
@@ -20,11 +21,6 @@ namespace {
 
 constexpr int PAGE = SPECA_KV_PAGE;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4_at8 __attribute__((ext_vector_type(4), aligned(8)));       // head size 72: rows of 72 bytes
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -33,29 +29,12 @@ union Frag {
   bf16x8 v;
 };
 
-__device__ inline uint32_t cvt_pk_bf16(float a, float b) {
-  const bf16x2 r = __builtin_convertvector(floatx2{a, b}, bf16x2);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-__device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 // four e4m3 bytes x a power of two -> four bf16
 __device__ inline void widen(uint32_t b, float scale, uint32_t* out) {
   const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
   out[0] = *reinterpret_cast<const uint32_t*>(&lo);
   out[1] = *reinterpret_cast<const uint32_t*>(&hi);
 }
-// maximum over the lanes l % 16 + {0, 16, 32, 48}, which hold one row
-__device__ __forceinline__ float max_of_groups(float x) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float sum_of_groups(float x) {
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
-}
-
 struct Args {
   const uint8_t *k, *v;
   const float *k_scale, *v_scale;

@@ -15,35 +15,18 @@
 // (32x32x16).  head_dim is padded with zeros to whole instructions (results that are not stored).
 #include <type_traits>
 
+#include "attn_lane.h"
 #include "gemm.h"
+#include "operators.h"
 
 namespace speca {
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx16 __attribute__((ext_vector_type(16)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-
 union Frag {
   uint4 u;
   bf16x8 v;
 };
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-
-// two floats -> packed bf16 pair, round to nearest even (one v_cvt_pk_bf16_f32)
-__device__ inline uint32_t cvt_pk_bf16(float a, float b) {
-  const floatx2 f = {a, b};
-  const bf16x2 r = __builtin_convertvector(f, bf16x2);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-
-// 2^x by the hardware instruction alone (inputs are <= 0 here; results below the normal range flush
-// to 0, -inf gives 0): exp2f() wraps it in range checks and a rescale, ~5 vector instructions per value.
-__device__ inline float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Transposed value tile in LDS: row = head dimension d, NK keys per row, rows unpadded.  The second
 // MFMA wants, per lane and 16-key step t, the keys 16t + 4h + {0..3} and 16t + 8 + 4h + {0..3}
@@ -104,8 +87,6 @@ __device__ inline void vt_write_off(int d, int kb, int* lo, int* hi) {
 // the same schedule faster on zeros (1490) and slower on data where rounds end ragged (13 632 tokens 2306 -> 2160 us); 8 waves
 // on one pair of tiles gain 6 % at 4608 tokens and lose 4 % at 27 286 and 13 % at 4096; the loads as inline assembly, without
 // the wait that the compiler puts ahead of a tile's value reads: 0.5 %.
-typedef short short4v __attribute__((ext_vector_type(4)));
-
 // element offset inside a row of the stored chunk c of row r (involutions: the loader uses them the other way round)
 template <int HD>
 __device__ inline int key_chunk(int c, int r) {
@@ -132,21 +113,20 @@ __device__ __forceinline__ void buffer_to_lds(const uint16_t* buffer, int bytes,
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
 }
 
-// maximum and sum over the lanes l % 16 + {0, 16, 32, 48}, which hold one query
-__device__ __forceinline__ float max_of_groups(float x) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float sum_of_groups(float x) {
-  x += __shfl_xor(x, 16, 64);
-  return x + __shfl_xor(x, 32, 64);
-}
+// Rows of equal length (PLAIN), or packed sequences, of which causal tokens see themselves and those before them.
+enum { PLAIN = 0, PACKED = 1, CAUSAL = 2 };
+struct TileArgs {
+  const uint16_t *q, *k, *v;
+  uint16_t* out;
+  int64_t ldq, ldk, ldv, ldo;       // elements from one token to the next
+  int32_t T, H, group;              // PLAIN: tokens of a row; query heads, of a key head
+  Packed seqs;
+  int32_t tiles;                    // PACKED, CAUSAL: blocks of a head
+  float scale_log2e;
+};
 
-template <int HD>
-__global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* __restrict__ qkv, uint16_t* __restrict__ out, int64_t ldo,
-                                                            int T, int H, float scale_log2e) {
+template <int HD, int MODE>
+__global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g) {
   constexpr int CH = HD / 8;                  // 16-byte chunks of a row, and load instructions of a tile
   constexpr int KS = (HD + 31) / 32;          // steps of 32 columns of q k^T
   constexpr int DT = (HD + 15) / 16;          // tiles of 16 dims of O^T
@@ -157,17 +137,39 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
   uint16_t* Vs = smem + 2 * TILE;             // [2][64][HD]
   uint16_t* zero = smem + 4 * TILE;           // head_dim 72: the key columns 72 .. 95 of the last step
 
-  // Blocks of a few queries (the last one of a (row, head) whose T ends shortly past a multiple of 128) come last: they are
-  // short and fill what the rounds of whole blocks leave.
-  const int nq = gridDim.x, pairs = gridDim.y * gridDim.z, lin = blockIdx.x + nq * (blockIdx.y + gridDim.y * blockIdx.z);
-  const int whole = T - (nq - 1) * 128 <= kFewQueries ? nq - 1 : nq;          // whole blocks per pair
-  const bool few = lin >= whole * pairs;
-  const int pair = few ? lin - whole * pairs : lin / whole, q0 = (few ? whole : lin - pair * whole) * 128;
-  const int row = pair / H, head = pair - row * H;
+  const float scale_log2e = g.scale_log2e;
+  int T, q0, head;
+  int64_t start;                              // of the sequence, in tokens
+  bool few;
+  if constexpr (MODE == PLAIN) {
+    // Blocks of a few queries (the last one of a (row, head) whose T ends shortly past a multiple of 128) come last: they are
+    // short and fill what the rounds of whole blocks leave.
+    T = g.T;
+    const int nq = gridDim.x, pairs = gridDim.y * gridDim.z, lin = blockIdx.x + nq * (blockIdx.y + gridDim.y * blockIdx.z);
+    const int whole = T - (nq - 1) * 128 <= kFewQueries ? nq - 1 : nq;          // whole blocks per pair
+    few = lin >= whole * pairs;
+    const int pair = few ? lin - whole * pairs : lin / whole;
+    q0 = (few ? whole : lin - pair * whole) * 128;
+    const int row = pair / g.H;
+    head = pair - row * g.H;
+    start = static_cast<int64_t>(row) * T;
+  } else {
+    head = blockIdx.x % g.H;
+    const int tile = blockIdx.x / g.H, seq = packed_find(g.seqs, tile, 1, 128, 0);
+    int at;
+    packed_rows(g.seqs, seq, &at, &T);
+    start = at;
+    q0 = (tile - packed_first_tile(g.seqs, seq, 1, 128, 0)) * 128;
+    if (q0 < 0 || q0 >= T) return;
+    few = T - q0 <= kFewQueries;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int64_t D = static_cast<int64_t>(H) * HD;
-  const uint16_t* base = qkv + static_cast<int64_t>(row) * T * 3 * D + head * HD;
+  const int kv_head = MODE == PLAIN ? head : head / g.group;
+  const uint16_t* qb = g.q + start * g.ldq + head * HD;
+  const uint16_t* kb = g.k + start * g.ldk + kv_head * HD;
+  const uint16_t* vb = g.v + start * g.ldv + kv_head * HD;
+  const int keys = MODE == CAUSAL && q0 + 128 < T ? q0 + 128 : T;               // that any query of the block sees
 
   bf16x8 qf[KS][2];                           // queries 16 n + l16, columns 32 ks + 8 g4 ..
 #pragma unroll
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       Frag f;
-      f.u = q < T && 4 * ks + g4 < CH ? *reinterpret_cast<const uint4*>(base + static_cast<int64_t>(q) * 3 * D + ks * 32 + g4 * 8) : make_uint4(0, 0, 0, 0);
+      f.u = q < T && 4 * ks + g4 < CH ? *reinterpret_cast<const uint4*>(qb + static_cast<int64_t>(q) * g.ldq + ks * 32 + g4 * 8) : make_uint4(0, 0, 0, 0);
       qf[ks][n] = f.v;
     }
   }
@@ -190,21 +192,22 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
   // Loader: wave w issues instructions i = w, w + 4, ... of a tile's CH; lane -> chunk slot 64 i + lane, row slot / CH.  Through
   // buffer descriptors that begin at the tile and end behind key T - 1: what lies beyond reads as zeros, and the compiler does not
   // take the loads for LDS reads that every later key fragment would have to wait for.
-  const int64_t row_bytes = 6 * D;
   uint32_t koff[LPW], voff[LPW];
 #pragma unroll
   for (int u = 0; u < LPW; ++u) {
     const int slot = (wave + 4 * u) * 64 + lane, r = static_cast<unsigned>(slot) / CH, p = slot - r * CH;
-    koff[u] = static_cast<uint32_t>(r * row_bytes + 2 * D + (key_chunk<HD>(p, r) << 4));
-    voff[u] = static_cast<uint32_t>(r * row_bytes + 4 * D + (value_chunk<HD>(p, r) << 4));
+    koff[u] = static_cast<uint32_t>(r * 2 * g.ldk + (key_chunk<HD>(p, r) << 4));
+    voff[u] = static_cast<uint32_t>(r * 2 * g.ldv + (value_chunk<HD>(p, r) << 4));
   }
-  auto issue = [&](int kt, uint16_t* dst, const uint32_t (&off)[LPW]) {
-    const int keys = T - kt * 64 < 64 ? T - kt * 64 : 64;
-    const uint16_t* from = base + kt * (32 * row_bytes);
+  auto issue = [&](const uint16_t* base, int64_t ld, int kt, uint16_t* dst, const uint32_t (&off)[LPW]) {
+    const int here = T - kt * 64 < 64 ? T - kt * 64 : 64;
+    const uint16_t* from = base + kt * (64 * ld);
 #pragma unroll
     for (int u = 0; u < LPW; ++u)
-      if (CH % 4 == 0 || wave + 4 * u < CH) buffer_to_lds(from, static_cast<int>(keys * row_bytes), off[u], dst + (kt & 1) * TILE + (wave + 4 * u) * 512);
+      if (CH % 4 == 0 || wave + 4 * u < CH) buffer_to_lds(from, static_cast<int>((here - 1) * 2 * ld) + 2 * HD, off[u], dst + (kt & 1) * TILE + (wave + 4 * u) * 512);
   };
+  auto issue_k = [&](int kt) { issue(kb, g.ldk, kt, Ks, koff); };
+  auto issue_v = [&](int kt) { issue(vb, g.ldv, kt, Vs, voff); };
   // a wave whose queries all lie beyond T only loads
   const bool active = q0 + wave * 32 < T;
 
@@ -237,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
       const float inv = 1.0f / sum[n];
       const int q = q0 + (few ? 0 : wave * 32) + n * 16 + l16;
       if (q < T) {
-        uint16_t* op = out + (static_cast<int64_t>(row) * T + q) * ldo + head * HD + 4 * g4;
+        uint16_t* op = g.out + (start + q) * g.ldo + head * HD + 4 * g4;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
           if (dt * 16 + 4 * g4 < HD)
@@ -281,10 +284,40 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
                       cvt_pk_bf16(s[2 * u + 1][n][0], s[2 * u + 1][n][1]), cvt_pk_bf16(s[2 * u + 1][n][2], s[2 * u + 1][n][3]));
     return pf.v;
   };
-  auto mask = [&](floatx4 (&s)[4][2], int kt) {                    // keys past T
+  // last key that query 16 n + l16 of the wave sees
+  auto last_key = [&](int n) {
+    const int q = q0 + (few ? 0 : wave * 32) + n * 16 + l16;
+    return MODE == CAUSAL && q < T ? q : T - 1;
+  };
+  auto mask = [&](floatx4 (&s)[4][2], int kt) {                    // keys past it
 #pragma unroll
     for (int i = 0; i < 32; ++i)
-      if (kt * 64 + (i >> 3) * 16 + 4 * g4 + (i & 3) >= T) s[i >> 3][(i >> 2) & 1][i & 3] = -INFINITY;
+      if (kt * 64 + (i >> 3) * 16 + 4 * g4 + (i & 3) > last_key((i >> 2) & 1)) s[i >> 3][(i >> 2) & 1][i & 3] = -INFINITY;
+  };
+  // A value that is no number must not meet the probability 0 of a causal query that does not see it.  Where the tile that a wave's queries see
+  // in part holds one, it is taken out of the product, and products of the places of +inf, -inf and NaN (among the words w of a fragment)
+  // with the places that a query sees say where it belongs.
+  auto odd_values = [&](const uint32_t* w, int words, auto&& product, floatx4& to) {
+    floatx4 hit[3];
+#pragma unroll
+    for (int kind = 0; kind < 3; ++kind) {
+      uint32_t at[4] = {};
+#pragma unroll
+      for (int i = 0; i < words; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t x = (w[i] >> (16 * h)) & 0xFFFFu;
+          const bool yes = kind == 0 ? x == 0x7F80u : kind == 1 ? x == 0xFF80u : (x & 0x7FFFu) > 0x7F80u;
+          at[i] |= yes ? 0x3F80u << (16 * h) : 0u;
+        }
+      hit[kind] = product(at);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (hit[0][e] > 0.0f) to[e] += INFINITY;
+      if (hit[1][e] > 0.0f) to[e] -= INFINITY;
+      if (hit[2][e] > 0.0f) to[e] = __uint_as_float(0x7FC00000u);
+    }
   };
 
   // Ring: keys are fetched two tiles ahead, values one.  At the top of tile kt the wave's outstanding loads are K(kt + 1) and V(kt);
@@ -299,19 +332,19 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
     asm volatile("" ::: "memory");                          \
     SPECA_PIN();                                            \
   }
-  const int ntiles = (T + 63) / 64;
+  const int ntiles = (keys + 63) / 64;
   if (few) {
     // At most 32 queries: the waves share them and split every tile's keys, 16 each, with statistics of their own (one after the
     // other in a single wave, the block would take half as long as a whole one).  Second contraction by 16x16x16 instructions.
     floatx4 s[2];
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
-    issue(0, Ks, koff);
-    issue(0, Vs, voff);
+    issue_k(0);
+    issue_v(0);
     for (int kt = 0; kt < ntiles; ++kt) {
       SPECA_TURN()
       if (kt + 1 < ntiles) {
-        issue(kt + 1, Ks, koff);
-        issue(kt + 1, Vs, voff);
+        issue_k(kt + 1);
+        issue_v(kt + 1);
       }
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
@@ -325,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
         float t = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if (kt * 64 + wave * 16 + 4 * g4 + i >= T) s[n][i] = -INFINITY;
+          if (kt * 64 + wave * 16 + 4 * g4 + i > last_key(n)) s[n][i] = -INFINITY;
           t = fmaxf(t, s[n][i]);
         }
         const float mnew = fmaxf(m[n], max_of_groups(t)), off = mnew == -INFINITY ? 0.0f : mnew * scale_log2e;      // no finite score yet: weights 0
@@ -346,9 +379,30 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
-        const short4v vf = value_half(kt & 1, 16 * wave, dt);
+        union { uint32_t u[2]; short4v v; } vf;
+        vf.v = value_half(kt & 1, 16 * wave, dt);
+        if (MODE == CAUSAL && kt + 1 == ntiles && __any((odd_halves(vf.u[0]) | odd_halves(vf.u[1])) != 0)) {
+          const uint32_t w[2] = {vf.u[0], vf.u[1]};
+          vf.u[0] = without_odd(w[0]);
+          vf.u[1] = without_odd(w[1]);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) o[dt][n] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, pf[n], o[dt][n], 0, 0, 0);
+          for (int n = 0; n < 2; ++n) {
+            o[dt][n] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf.v, pf[n], o[dt][n], 0, 0, 0);
+            odd_values(w, 2, [&](const uint32_t* at) {
+              union { uint32_t u[2]; short4v v; } a, b;
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const int key = kt * 64 + 16 * wave + 4 * g4 + 2 * i;
+                a.u[i] = at[i];
+                b.u[i] = (key <= last_key(n) ? 0x3F80u : 0u) | (key + 1 <= last_key(n) ? 0x3F800000u : 0u);
+              }
+              return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a.v, b.v, floatx4{}, 0, 0, 0);
+            }, o[dt][n]);
+          }
+          continue;
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) o[dt][n] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf.v, pf[n], o[dt][n], 0, 0, 0);
       }
     }
     // together: everything relative to the largest maximum, then waves 1 .. 3 hand their sums to wave 0 through LDS
@@ -400,6 +454,8 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
   // side, pinned around every pair of matrix instructions: first the scores of tile kt + 1 with the first NP probabilities of tile
   // kt, then O^T += V^T P^T with the other probabilities in its first half and the maximum of tile kt + 1 in its second.  Fragments
   // are read RA steps ahead.  NEXT: there is a tile kt + 1; the last one is masked.
+  // Of a block of causal queries the first two waves see no key of the last tile: they only load it.
+  const int own = MODE == CAUSAL ? min(ntiles, (q0 + wave * 32) / 64 + 1) : ntiles;          // tiles of this wave
   constexpr int NS = 4 * KS, NV = 2 * DT, RA = 4, NP = 20;
   auto tile = [&](floatx4 (&sc)[4][2], floatx4 (&sn)[4][2], int kt, int buf, auto next_tag) {
     constexpr bool NEXT = decltype(next_tag)::value;
@@ -418,6 +474,43 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
       }
     }
     psum[0] = psum[1] = 0.0f;
+    if constexpr (!NEXT && MODE == CAUSAL) {
+      union Words { bf16x8 v; uint32_t u[4]; };
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        Words x;
+        x.v = value_frag(buf, i / DT, i % DT);
+        any |= odd_halves(x.u[0]) | odd_halves(x.u[1]) | odd_halves(x.u[2]) | odd_halves(x.u[3]);
+      }
+      if (__any(any != 0)) {
+        probabilities(sc, 0, 32);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          Words x, y;
+          x.v = value_frag(buf, i / DT, i % DT);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) y.u[j] = without_odd(x.u[j]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            o[i % DT][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y.v, pack(sc, i / DT, n), o[i % DT][n], 0, 0, 0);
+            odd_values(x.u, 4, [&](const uint32_t* at) {
+              Words a, b;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const int key = kt * 64 + 32 * (i / DT) + 16 * (j >> 1) + 4 * g4 + 2 * (j & 1);
+                a.u[j] = at[j];
+                b.u[j] = (key <= last_key(n) ? 0x3F80u : 0u) | (key + 1 <= last_key(n) ? 0x3F800000u : 0u);
+              }
+              return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, floatx4{}, 0, 0, 0);
+            }, o[i % DT][n]);
+          }
+        }
+#pragma unroll
+        for (int n = 0; n < 2; ++n) lrun[n] += psum[n];
+        return;
+      }
+    }
     if constexpr (NEXT) {
 #pragma unroll
       for (int i = 0; i < NS; ++i) {
@@ -445,7 +538,7 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
       if (i + RA < NV) vf[i + RA] = value_frag(buf, (i + RA) / DT, (i + RA) % DT);
       if (i >= DT - 1 && i <= DT) pf[1][i - DT + 1] = pack(sc, 1, i - DT + 1);
       if constexpr (NEXT) {
-        if (i == DT && kt * 64 + 128 > T) mask(sn, kt + 1);
+        if (i == DT && (MODE == CAUSAL ? kt + 2 == own : kt * 64 + 128 > T)) mask(sn, kt + 1);
       }
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
@@ -464,15 +557,15 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
 #define SPECA_ATTN_TILE(PAR, SC, SN)                                      \
   {                                                                       \
     SPECA_TURN()                                                          \
-    if (kt + 2 < ntiles) issue(kt + 2, Ks, koff);                         \
-    issue(kt + 1, Vs, voff);                                              \
+    if (kt + 2 < ntiles) issue_k(kt + 2);                         \
+    issue_v(kt + 1);                                              \
     if (active) tile(SC, SN, kt, PAR, std::true_type());                  \
   }
   floatx4 sa[4][2], sb[4][2];
-  issue(0, Ks, koff);
+  issue_k(0);
   SPECA_TURN()
-  if (1 < ntiles) issue(1, Ks, koff);
-  issue(0, Vs, voff);
+  if (1 < ntiles) issue_k(1);
+  issue_v(0);
   if (active) {
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
@@ -480,18 +573,18 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
 #pragma unroll
       for (int n = 0; n < 2; ++n) sa[i & 3][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i >> 2][n], i < 4 ? floatx4{} : sa[i & 3][n], 0, 0, 0);
     }
-    if (ntiles == 1) mask(sa, 0);
+    if (own == 1) mask(sa, 0);
     tmax[0] = tmax[1] = -INFINITY;
     maximum(sa, 0, 32);
     reference();
   }
   int kt = 0;
-  for (; kt + 2 < ntiles; ++kt) {
+  for (; kt + 2 < own; ++kt) {
     SPECA_ATTN_TILE(0, sa, sb)
     ++kt;
     SPECA_ATTN_TILE(1, sb, sa)
   }
-  if (kt + 1 < ntiles) {
+  if (kt + 1 < own) {
     SPECA_ATTN_TILE(0, sa, sb)
     ++kt;
 #pragma unroll
@@ -500,7 +593,9 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const uint16_t* _
       for (int n = 0; n < 2; ++n) sa[m][n] = sb[m][n];
   }
   SPECA_TURN()
+  if (MODE == CAUSAL && kt + 1 < ntiles) issue_v(kt + 1);         // the other two waves' last tile
   if (active) tile(sa, sb, kt, kt & 1, std::false_type());
+  if (MODE == CAUSAL && own < ntiles) SPECA_TURN()
 #undef SPECA_ATTN_TILE
 #undef SPECA_TURN
 #undef SPECA_PIN
@@ -757,12 +852,43 @@ Error launch_hd(const void* qkv, void* out, int64_t ldo, int rows, int T, int H,
     return ok();
   }
   const float sl2 = 1.4426950408889634f / sqrtf(static_cast<float>(HD));
-  attention_dma_kernel<HD><<<dim3((T + 127) / 128, H, rows), 256, 0, st>>>(static_cast<const uint16_t*>(qkv), static_cast<uint16_t*>(out), ldo, T, H, sl2);
+  const uint16_t* q = static_cast<const uint16_t*>(qkv);
+  const int64_t D = static_cast<int64_t>(H) * HD;
+  const TileArgs g = {q, q + D, q + 2 * D, static_cast<uint16_t*>(out), 3 * D, 3 * D, 3 * D, ldo, T, H, 1, {}, 0, sl2};
+  attention_dma_kernel<HD, PLAIN><<<dim3((T + 127) / 128, H, rows), 256, 0, st>>>(g);
+  SPECA_HIP(hipGetLastError());
+  return ok();
+}
+
+template <int HD>
+Error launch_packed_hd(const PackedAttention& a, hipStream_t st) {
+  const int64_t tiles = packed_tiles(a.seqs, 1, 128, 0), blocks = tiles * a.heads;
+  if (blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "speca_attention_packed: %d tokens of %d heads are too many for one call", a.seqs.total, a.heads);
+  const TileArgs g = {static_cast<const uint16_t*>(a.q), static_cast<const uint16_t*>(a.k), static_cast<const uint16_t*>(a.v), static_cast<uint16_t*>(a.out),
+                      a.ldq, a.ldk, a.ldv, a.ldo, 0, a.heads, a.heads / a.kv_heads, a.seqs, static_cast<int32_t>(tiles), 1.4426950408889634f * a.scale};
+  if (a.causal) attention_dma_kernel<HD, CAUSAL><<<static_cast<unsigned>(blocks), 256, 0, st>>>(g);
+  else attention_dma_kernel<HD, PACKED><<<static_cast<unsigned>(blocks), 256, 0, st>>>(g);
   SPECA_HIP(hipGetLastError());
   return ok();
 }
 
 }  // namespace
+
+// 16-byte pieces of q, k and v, 8-byte ones of the output; a tile of 64 keys within the 2 GiB that a buffer's offsets reach
+bool attention_packed_mfma_supported(const PackedAttention& a) {
+  const uintptr_t in = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v);
+  return (a.head_dim == 64 || a.head_dim == 72 || a.head_dim == 128) && in % 16 == 0 && (a.ldq | a.ldk | a.ldv) % 8 == 0 &&
+         reinterpret_cast<uintptr_t>(a.out) % 8 == 0 && a.ldo % 4 == 0 && a.ldk < (int64_t{1} << 23) && a.ldv < (int64_t{1} << 23);
+}
+
+Error launch_attention_packed_mfma(const PackedAttention& a, hipStream_t st) {
+  switch (a.head_dim) {
+    case 64: return launch_packed_hd<64>(a, st);
+    case 72: return launch_packed_hd<72>(a, st);
+    case 128: return launch_packed_hd<128>(a, st);
+  }
+  SPECA_FAIL(SPECA_EUNSUPPORTED, "attention: head_dim %d has no MFMA kernel", a.head_dim);
+}
 
 bool attention_mfma_supported(const void* qkv, const void* out, int64_t ldo, int H, int hd) {
   return (hd == 64 || hd == 72 || hd == 128) && ldo % 4 == 0 && reinterpret_cast<uintptr_t>(qkv) % 16 == 0 && reinterpret_cast<uintptr_t>(out) % 8 == 0;

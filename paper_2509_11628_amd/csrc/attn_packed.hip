@@ -24,6 +24,7 @@ Error launch_attention_packed(int dtype, const PackedAttention& given, hipStream
   if (!(a.scale >= 0.0f) || !std::isfinite(a.scale)) SPECA_FAIL(SPECA_EINVAL, "%s: scale = %g", who, a.scale);
   if (a.seqs.total == 0) return ok();
   if (a.scale == 0.0f) a.scale = 1.0f / std::sqrt(static_cast<float>(a.head_dim));
+  if (dtype == SPECA_BF16 && attention_packed_mfma_supported(a)) return launch_attention_packed_mfma(a, st);
   return launch_attention_packed_f32(dtype, a, st);
 }
 

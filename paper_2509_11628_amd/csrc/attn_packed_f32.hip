@@ -5,21 +5,15 @@
 // operand of the O^T product as it stands (instruction r takes keys 4 q + r).  The head dimension is dealt to the 16-row tiles of O^T in pieces
 // of four (tile i % 4 of group i / 4 owns dimensions 64 g + 4 row + i), so a lane's values are 16-byte pieces of V and of the output.
 // T = storage type of q, k, v and the output; arithmetic is fp32.
+#include "attn_lane.h"
 #include "operators.h"
 
 namespace speca {
 
 namespace {
 
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ floatx4 mfma4(float a, float b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
-__device__ inline uint32_t cvt_pk_bf16(float a, float b) {      // to nearest even, NaN stays NaN
-  const bf16x2 r = __builtin_convertvector(floatx2{a, b}, bf16x2);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
 template <bool WIDE>
 __device__ inline floatx4 ld_quad(const float* p) {
   if constexpr (WIDE) return *reinterpret_cast<const floatx4*>(p);

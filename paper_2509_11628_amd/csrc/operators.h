@@ -26,7 +26,10 @@ struct PackedAttention {
   float scale;
 };
 Error launch_attention_packed(int dtype, const PackedAttention& a, hipStream_t st);
-// On the fp32 matrix instructions, arguments checked, scale given.
+// The kernels behind it, arguments checked, scale given: bf16 tiles (attn_mfma.hip) where alignment and strides allow, the fp32 matrix
+// instructions otherwise.
+bool attention_packed_mfma_supported(const PackedAttention& a);
+Error launch_attention_packed_mfma(const PackedAttention& a, hipStream_t st);
 Error launch_attention_packed_f32(int dtype, const PackedAttention& a, hipStream_t st);
 
 Error check_kv_cache(const char* who, const speca_kv_cache& c, const speca_kv_table& t);

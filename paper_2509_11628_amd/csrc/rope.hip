@@ -9,6 +9,7 @@
 #include <cmath>
 
 #include "gemm.h"
+#include "attn_lane.h"
 #include "operators.h"
 
 namespace speca {
@@ -17,12 +18,6 @@ namespace {
 
 constexpr int kMaxHead = 128;
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float floatx2 __attribute__((ext_vector_type(2)));
-__device__ inline uint32_t cvt_pk_bf16(float a, float b) {      // to nearest even, NaN stays NaN
-  const bf16x2 r = __builtin_convertvector(floatx2{a, b}, bf16x2);
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
 
 struct RopeSide {
   const void* x;
