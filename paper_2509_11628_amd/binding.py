@@ -263,33 +263,49 @@ def attention(qkv, heads: int, out=None):
 
 def _heads(name, x, like=None):
     """A tensor [tokens, heads, head_dim] whose heads lie one after the other: its distance between tokens."""
-    import torch
-    if x.dim() != 3 or x.stride(2) != 1 and x.shape[2] > 1 or x.stride(1) != x.shape[2] and x.shape[1] > 1:
-        raise ValueError(f"{name}: [tokens, heads, head_dim] with the heads of a token in one piece is wanted, got {tuple(x.shape)} with strides {x.stride()}")
-    if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32):
-        raise ValueError(f"{name}: a bf16 or fp32 device tensor is wanted, got {x.dtype} on {x.device}")
-    if like is not None and (x.dtype != like.dtype or x.device != like.device):
+    shape, stride = x.shape, x.stride()
+    if len(shape) != 3 or (stride[2] != 1 and shape[2] > 1) or (stride[1] != shape[2] and shape[1] > 1):
+        raise ValueError(f"{name}: [tokens, heads, head_dim] with the heads of a token in one piece is wanted, got {tuple(shape)} with strides {stride}")
+    if like is None:
+        if not x.is_cuda or x.dtype not in _storage_types():
+            raise ValueError(f"{name}: a bf16 or fp32 device tensor is wanted, got {x.dtype} on {x.device}")
+    elif x.dtype is not like.dtype or x.device != like.device:
         raise ValueError(f"{name}: {x.dtype} on {x.device}, the others are {like.dtype} on {like.device}")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1] * x.shape[2]
+    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
 
-def _ints(name, x, shape, like):
-    """A contiguous int32 tensor on the device of `like`; None in `shape`: any size."""
+_dtypes = None
+
+
+def _storage_types():
+    """torch types the library takes, and its names for them."""
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {torch.bfloat16: BF16, torch.float32: F32}
+    return _dtypes
+
+
+def _ints(name, x, like, dims, rows=None, cols=None):
+    """Address of a contiguous int32 tensor of one or two dimensions on the device of `like`, with as many rows and columns where they are given."""
     import torch
-    if x.dtype != torch.int32 or x.device != like.device or not x.is_contiguous() or x.dim() != len(shape) or any(
-            n is not None and n != m for n, m in zip(shape, x.shape)):
-        raise ValueError(f"{name}: contiguous int32 {shape} on {like.device} is wanted, got {x.dtype} {tuple(x.shape)} on {x.device}")
+    shape = x.shape
+    if (x.dtype is not torch.int32 or x.device != like.device or len(shape) != dims or not x.is_contiguous()
+            or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols)):
+        want = [n if n is not None else "any" for n in (rows, cols)[:dims]]
+        raise ValueError(f"{name}: contiguous int32 {want} on {like.device} is wanted, got {x.dtype} {tuple(shape)} on {x.device}")
     return x.data_ptr()
 
 
 def _stand_alone(like, name, *args):
     """Call an entry point without a context on the current stream of `like`'s device."""
     import torch
-    lib = load_library()
-    if like.device.index != torch.cuda.current_device():
-        with torch.cuda.device(like.device):
+    lib, device = load_library(), like.get_device()
+    if device != torch.cuda.current_device():
+        with torch.cuda.device(device):
             return _stand_alone(like, name, *args)
-    code = getattr(lib, name)(torch.cuda.current_stream().cuda_stream, BF16 if like.dtype == torch.bfloat16 else F32, *args)
+    # the stream's handle without a torch.cuda.Stream around it, which takes longer than the launch
+    code = getattr(lib, name)(torch._C._cuda_getCurrentRawStream(device), _storage_types()[like.dtype], *args)
     if code != OK:
         raise SpecaError(code, lib.speca_last_error(None).decode())
 
@@ -299,12 +315,10 @@ def make_rope(dims, theta=10000.0, scale=1.0, pairing=ROPE_ADJACENT, spectrum=RO
     n = len(dims)
     if not 1 <= n <= ROPE_MAX_AXES:
         raise ValueError(f"1 to {ROPE_MAX_AXES} axes, got {n}")
-    per = [list(v) if isinstance(v, (list, tuple)) else [v] * n for v in (theta, scale)]
-    if any(len(v) != n for v in per):
+    theta, scale = (tuple(v) if isinstance(v, (list, tuple)) else (v,) * n for v in (theta, scale))
+    if len(theta) != n or len(scale) != n:
         raise ValueError("theta and scale: one number, or one per axis")
-    pad = [0] * (ROPE_MAX_AXES - n)
-    return Rope(n, (C.c_int32 * ROPE_MAX_AXES)(*dims, *pad), (C.c_float * ROPE_MAX_AXES)(*per[0], *pad), (C.c_float * ROPE_MAX_AXES)(*per[1], *pad),
-                pairing, spectrum)
+    return Rope(n, tuple(dims), theta, scale, pairing, spectrum)
 
 
 def rope_axes(rope: Rope, positions, q, k=None, q_norm=None, k_norm=None, eps: float = 1e-6, out=None):
@@ -315,7 +329,7 @@ def rope_axes(rope: Rope, positions, q, k=None, q_norm=None, k_norm=None, eps: f
     for i, (name, x, norm) in enumerate((("q", q, q_norm), ("k", k, k_norm))):
         if x is None:
             continue
-        ldx = _heads(name, x, q)
+        ldx = _heads(name, x, q if i else None)
         if x.shape[0] != q.shape[0] or x.shape[2] != q.shape[2]:
             raise ValueError(f"{name}: {tuple(x.shape)}, q is {tuple(q.shape)}")
         if norm is not None and (norm.dtype != q.dtype or norm.device != q.device or tuple(norm.shape) != (q.shape[2],) or not norm.is_contiguous()):
@@ -327,7 +341,7 @@ def rope_axes(rope: Rope, positions, q, k=None, q_norm=None, k_norm=None, eps: f
         made.append(o)
         sides.append(RopeIO(x.data_ptr(), o.data_ptr(), None if norm is None else norm.data_ptr(), ldx, ldo, x.shape[1]))
     if q.shape[0]:
-        _stand_alone(q, "speca_rope_axes", rope, _ints("positions", positions, (q.shape[0], rope.axes), q), q.shape[0], q.shape[2], eps, sides[0],
+        _stand_alone(q, "speca_rope_axes", rope, _ints("positions", positions, q, 2, q.shape[0], rope.axes), q.shape[0], q.shape[2], eps, sides[0],
                      sides[1] if len(sides) > 1 else None)
     return tuple(made) if len(made) > 1 else made[0]
 
@@ -344,7 +358,7 @@ def attention_packed(q, k, v, starts, causal: bool = False, scale: float = 0.0, 
     ldo = _heads("out", out, q)
     if out.shape != q.shape:
         raise ValueError(f"out: {tuple(out.shape)}, q is {tuple(q.shape)}")
-    at = _ints("starts", starts, (None,), q)
+    at = _ints("starts", starts, q, 1)
     if q.shape[0]:
         _stand_alone(q, "speca_attention_packed", q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, out.data_ptr(), ldo, at, len(starts) - 1,
                      q.shape[0], q.shape[1], k.shape[1], q.shape[2], int(causal), scale)
@@ -362,7 +376,8 @@ class KVCache:
             raise ValueError(f"pages {tuple(k.shape)} and {tuple(v.shape)} with scales {tuple(k_scale.shape)} and {tuple(v_scale.shape)} do not fit")
         if k.dtype != torch.uint8 or v.dtype != torch.uint8 or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
             raise ValueError("pages are uint8, their scales fp32")
-        if not all(x.is_cuda and x.is_contiguous() and x.device == k.device for x in (k, v, k_scale, v_scale)):
+        if not (k.is_cuda and k.device == v.device == k_scale.device == v_scale.device and k.is_contiguous() and v.is_contiguous()
+                and k_scale.is_contiguous() and v_scale.is_contiguous()):
             raise ValueError("pages and scales are contiguous tensors on one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.desc = KVCacheDesc(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), p, h, hd)
@@ -382,7 +397,7 @@ def _cached(cache, x, table, first, starts, first_name):
         raise ValueError(f"tokens on {x.device}, the cache is on {cache.k.device}")
     if x.shape[2] != cache.k.shape[3]:
         raise ValueError(f"heads of {x.shape[2]}, the cache's have {cache.k.shape[3]}")
-    return KVTable(_ints("table", table, (n, None), x), table.shape[1]), _ints(first_name, first, (n,), x), _ints("starts", starts, (None,), x), n
+    return KVTable(_ints("table", table, x, 2, n), table.shape[1]), _ints(first_name, first, x, 1, n), _ints("starts", starts, x, 1), n
 
 
 def kv_store(cache: KVCache, table, past, k, v, starts):

@@ -73,8 +73,9 @@ __device__ inline void rope_write(bf16_t* p, const float (&v)[VP]) {
 // One wave = one token and heads_per_wave of its heads; a lane owns VP pairs of a head and a wave's lanes hold 64 / lanes_per_head heads at a
 // time.  The pieces of a lane are VP features at lo and VP at hi: with HALVES the two sides of its pairs, otherwise neighbours, of which
 // features 2j and 2j + 1 are a pair.
-template <typename T, int VP, bool HALVES>
+template <typename T, int VP, bool HALVES, bool NORM>
 __global__ __launch_bounds__(256) void rope_axes_kernel(const RopeArgs g) {
+  constexpr int UN = 4;
   const int lane = threadIdx.x & 63;
   const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int64_t tok = item / g.chunks;
@@ -86,6 +87,22 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const RopeArgs g) {
   int lo = u * 2 * VP, hi = lo + VP;
   if (HALVES && u * VP < pairs) { lo = u * VP; hi = pairs + lo; }
 
+  const bool has_q = g.side[0].norm != nullptr, has_k = g.side[1].norm != nullptr;
+  float wq[2 * VP] = {}, wk[2 * VP] = {};
+  if (NORM && live) {
+    float w[VP];
+    const T* const from[2] = {static_cast<const T*>(g.side[0].norm), static_cast<const T*>(g.side[1].norm)};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (!(i ? has_k : has_q)) continue;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        rope_read<VP>(from[i] + (half ? hi : lo), w);
+#pragma unroll
+        for (int j = 0; j < VP; ++j) (i ? wk : wq)[half * VP + j] = w[j];
+      }
+    }
+  }
   float cs[VP], sn[VP];
 #pragma unroll
   for (int j = 0; j < VP; ++j) {
@@ -97,52 +114,97 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const RopeArgs g) {
       sincospif(2.0f * static_cast<float>(turns - rint(turns)), &sn[j], &cs[j]);
     }
   }
+  // UN groups of heads at a time: that many loads are on their way before the first is waited for
   const int end = min(g.total_heads, (chunk + 1) * g.heads_per_wave);
-  for (int h = chunk * g.heads_per_wave + sub; h < end; h += per) {
-    const RopeSide& s = g.side[h < g.heads ? 0 : 1];
-    const int64_t at = static_cast<int64_t>(h < g.heads ? h : h - g.heads) * g.hd;
-    const T* x = static_cast<const T*>(s.x) + tok * s.ldx + at;
-    T* out = static_cast<T*>(s.out) + tok * s.ldo + at;
-    float a[VP] = {}, b[VP] = {};
-    if (live) { rope_read<VP>(x + lo, a); rope_read<VP>(x + hi, b); }
-    if (s.norm) {
-      float sum = 0.0f;
+  for (int h0 = chunk * g.heads_per_wave + sub; h0 < end; h0 += UN * per) {
+    float a[UN][VP], b[UN][VP];
 #pragma unroll
-      for (int j = 0; j < VP; ++j) sum += a[j] * a[j] + b[j] * b[j];
-      for (int off = g.lanes_per_head >> 1; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
-      const float r = 1.0f / sqrtf(sum / static_cast<float>(g.hd) + g.eps);
-      float wa[VP] = {}, wb[VP] = {};
-      if (live) { rope_read<VP>(static_cast<const T*>(s.norm) + lo, wa); rope_read<VP>(static_cast<const T*>(s.norm) + hi, wb); }
+    for (int i = 0; i < UN; ++i) {
+      const int h = h0 + i * per;
 #pragma unroll
-      for (int j = 0; j < VP; ++j) { a[j] *= r * wa[j]; b[j] *= r * wb[j]; }
-    }
-    if (!live) continue;
-    if constexpr (HALVES || VP == 1) {
-#pragma unroll
-      for (int j = 0; j < VP; ++j) {
-        const float c = a[j] * cs[j] - b[j] * sn[j];
-        b[j] = a[j] * sn[j] + b[j] * cs[j];
-        a[j] = c;
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < VP; j += 2) {
-        const float c = a[j] * cs[j / 2] - a[j + 1] * sn[j / 2], d = b[j] * cs[VP / 2 + j / 2] - b[j + 1] * sn[VP / 2 + j / 2];
-        a[j + 1] = a[j] * sn[j / 2] + a[j + 1] * cs[j / 2];
-        b[j + 1] = b[j] * sn[VP / 2 + j / 2] + b[j + 1] * cs[VP / 2 + j / 2];
-        a[j] = c;
-        b[j] = d;
+      for (int j = 0; j < VP; ++j) a[i][j] = b[i][j] = 0.0f;
+      if (live && h < end) {
+        const RopeSide& s = g.side[h < g.heads ? 0 : 1];
+        const T* x = static_cast<const T*>(s.x) + tok * s.ldx + static_cast<int64_t>(h < g.heads ? h : h - g.heads) * g.hd;
+        rope_read<VP>(x + lo, a[i]);
+        rope_read<VP>(x + hi, b[i]);
       }
     }
-    rope_write<VP>(out + lo, a);
-    rope_write<VP>(out + hi, b);
+    if (NORM) {
+      float sum[UN];
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        // pair by pair, then pairs 1, 2, 4, ... apart: the same order, and the same bits, whether a lane holds one pair or four
+        if constexpr (VP == 1) {
+          sum[i] = fmaf(a[i][0], a[i][0], b[i][0] * b[i][0]);
+        } else {
+          const bool across = HALVES && u * VP < pairs;
+          float t[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float x = across ? a[i][j] : j < 2 ? a[i][2 * j] : b[i][2 * j - 4], y = across ? b[i][j] : j < 2 ? a[i][2 * j + 1] : b[i][2 * j - 3];
+            t[j] = fmaf(x, x, y * y);
+          }
+          sum[i] = (t[0] + t[1]) + (t[2] + t[3]);
+        }
+      }
+      for (int off = 1; off < g.lanes_per_head; off <<= 1)
+#pragma unroll
+        for (int i = 0; i < UN; ++i) sum[i] += __shfl_xor(sum[i], off, 64);
+#pragma unroll
+      for (int i = 0; i < UN; ++i) {
+        const bool of_q = h0 + i * per < g.heads;
+        const float r = rsqrtf(sum[i] / static_cast<float>(g.hd) + g.eps);
+        if (of_q ? has_q : has_k) {
+#pragma unroll
+          for (int j = 0; j < VP; ++j) { a[i][j] *= r * (of_q ? wq[j] : wk[j]); b[i][j] *= r * (of_q ? wq[VP + j] : wk[VP + j]); }
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < UN; ++i) {
+      const int h = h0 + i * per;
+      if (!live || h >= end) continue;
+      float(&p)[VP] = a[i];
+      float(&q)[VP] = b[i];
+      if constexpr (HALVES || VP == 1) {
+#pragma unroll
+        for (int j = 0; j < VP; ++j) {
+          const float c = fmaf(p[j], cs[j], -(q[j] * sn[j]));
+          q[j] = fmaf(p[j], sn[j], q[j] * cs[j]);
+          p[j] = c;
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < VP; j += 2) {
+          const float c = fmaf(p[j], cs[j / 2], -(p[j + 1] * sn[j / 2])), d = fmaf(q[j], cs[VP / 2 + j / 2], -(q[j + 1] * sn[VP / 2 + j / 2]));
+          p[j + 1] = fmaf(p[j], sn[j / 2], p[j + 1] * cs[j / 2]);
+          q[j + 1] = fmaf(q[j], sn[VP / 2 + j / 2], q[j + 1] * cs[VP / 2 + j / 2]);
+          p[j] = c;
+          q[j] = d;
+        }
+      }
+      const RopeSide& s = g.side[h < g.heads ? 0 : 1];
+      T* out = static_cast<T*>(s.out) + tok * s.ldo + static_cast<int64_t>(h < g.heads ? h : h - g.heads) * g.hd;
+      rope_write<VP>(out + lo, p);
+      rope_write<VP>(out + hi, q);
+    }
   }
 }
 
+template <typename T, int VP>
+void launch_vp(const RopeArgs& g, bool halves, unsigned blocks, hipStream_t st) {
+  const bool norm = g.side[0].norm || g.side[1].norm;
+  if (halves && norm) rope_axes_kernel<T, VP, true, true><<<blocks, 256, 0, st>>>(g);
+  else if (halves) rope_axes_kernel<T, VP, true, false><<<blocks, 256, 0, st>>>(g);
+  else if (norm) rope_axes_kernel<T, VP, false, true><<<blocks, 256, 0, st>>>(g);
+  else rope_axes_kernel<T, VP, false, false><<<blocks, 256, 0, st>>>(g);
+}
+
 template <typename T>
-void launch_t(const RopeArgs& g, bool halves, unsigned blocks, hipStream_t st) {
-  if (halves) rope_axes_kernel<T, 1, true><<<blocks, 256, 0, st>>>(g);
-  else rope_axes_kernel<T, 1, false><<<blocks, 256, 0, st>>>(g);
+void launch_t(const RopeArgs& g, int vp, bool halves, unsigned blocks, hipStream_t st) {
+  if (vp == 4) launch_vp<T, 4>(g, halves, blocks, st);
+  else launch_vp<T, 1>(g, halves, blocks, st);
 }
 
 Error check_side(const char* name, int dtype, const speca_rope_io& s, int hd) {
@@ -205,16 +267,27 @@ Error launch_rope_axes(int dtype, const speca_rope& rope, const int32_t* positio
       g.axis[pair] = static_cast<uint8_t>(a);
     }
   }
+  // Four pairs a lane where every piece of four features lies at a whole piece (16 bytes in fp32, 8 in bf16), one pair otherwise: clip below 150
+  // against 600 us.  With HALVES the pairs of a lane must end with the rotation, and what does not turn has to be whole lanes too.
+  const size_t piece = 4 * dtype_size(dtype);
+  uintptr_t at = 0;
+  for (const RopeSide& s : g.side)
+    at |= reinterpret_cast<uintptr_t>(s.x) | reinterpret_cast<uintptr_t>(s.out) | reinterpret_cast<uintptr_t>(s.norm) | static_cast<uintptr_t>(s.ldx * dtype_size(dtype)) |
+          static_cast<uintptr_t>(s.ldo * dtype_size(dtype));
+  const bool halves = rope.pairing == SPECA_ROPE_HALVES;
+  const int vp = at % piece == 0 && head_dim % 8 == 0 && (!halves || rotated % 8 == 0) ? 4 : 1;
   g.lanes_per_head = 1;
-  while (g.lanes_per_head < head_dim / 2 && g.lanes_per_head < 64) g.lanes_per_head *= 2;
-  const int per = 64 / g.lanes_per_head;
-  const int steps = (g.total_heads + per - 1) / per;
-  g.chunks = steps;
-  g.heads_per_wave = per;
+  while (g.lanes_per_head < head_dim / (2 * vp)) g.lanes_per_head *= 2;
+  // A wave takes all heads of its token where there are tokens enough for 8 waves per SIMD; with fewer, the heads are dealt to as many waves.
+  const int per = 64 / g.lanes_per_head, steps = (g.total_heads + per - 1) / per;
+  const int64_t waves = int64_t{32} * compute_units();
+  g.chunks = static_cast<int>(std::min<int64_t>(steps, std::max<int64_t>(1, (waves + tokens - 1) / tokens)));
+  g.heads_per_wave = (steps + g.chunks - 1) / g.chunks * per;
+  g.chunks = (g.total_heads + g.heads_per_wave - 1) / g.heads_per_wave;
   const int64_t blocks = (tokens * g.chunks + 3) / 4;
   if (blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: %lld tokens are too many for one call", static_cast<long long>(tokens));
-  if (dtype == SPECA_BF16) launch_t<bf16_t>(g, rope.pairing == SPECA_ROPE_HALVES, static_cast<unsigned>(blocks), st);
-  else launch_t<float>(g, rope.pairing == SPECA_ROPE_HALVES, static_cast<unsigned>(blocks), st);
+  if (dtype == SPECA_BF16) launch_t<bf16_t>(g, vp, halves, static_cast<unsigned>(blocks), st);
+  else launch_t<float>(g, vp, halves, static_cast<unsigned>(blocks), st);
   SPECA_HIP(hipGetLastError());
   return ok();
 }
