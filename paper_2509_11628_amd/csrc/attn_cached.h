@@ -1,0 +1,132 @@
+// What the kernels of attention over 8-bit pages share: their arguments, how the work is dealt, and widening.
+#pragma once
+
+#include "attn_lane.h"
+#include "operators.h"
+
+namespace speca {
+
+constexpr int PAGE = SPECA_KV_PAGE;
+
+// four e4m3 bytes x a power of two -> four bf16
+__device__ inline void widen(uint32_t b, float scale, uint32_t* out) {
+  const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+  out[0] = *reinterpret_cast<const uint32_t*>(&lo);
+  out[1] = *reinterpret_cast<const uint32_t*>(&hi);
+}
+struct CachedArgs {
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;
+  const uint16_t* q;
+  uint16_t* out;
+  int64_t ldq, ldo;
+  Packed seqs;
+  const int32_t *lens, *table;
+  float *part, *stats;              // of splits, by slot: O [rows of a tile][HD], and maximum and sum [2][rows]
+  int32_t table_ld, pages, kv_heads, group;
+  int32_t max_len, resident, least_pages, slots;
+  int32_t causal, wide;             // wide: queries at whole 16 bytes, outputs at whole 8
+  float scale_log2e;
+};
+
+// How the work is dealt.  The host knows no lengths, so every wave works it out from the lists on the device, 64 sequences at a time.  A unit is
+// one row tile of one key head over one split of its sequence's range of pages.  With `whole` units if nothing is split and W pages to visit in
+// all, ranges longer than split_pages = W / E are split evenly, which makes at most min(W / split_pages + whole, 2 W / split_pages) units of split ranges:
+//   whole <= resident / 4:  E = resident - whole             one round of the blocks that fit on the chip, none idle for long
+//   otherwise:              E = max(4 resident - whole, 2 resident)  four rounds, so that the last one, which is not full, costs little
+// and never more than 4 resident of them, which is what the workspace has room for.
+struct Deal {
+  int tiles, pages;                 // of the lane's sequence in the first 64
+  int64_t units;                    // of all
+  int split_pages;
+};
+template <int ROWS>
+__device__ inline void deal_sequence(const CachedArgs& g, int s, int* tiles, int* pages) {
+  *tiles = *pages = 0;
+  if (s >= g.seqs.n) return;
+  int start, n;
+  packed_rows(g.seqs, s, &start, &n);
+  const int len = g.lens[s];
+  *tiles = static_cast<int>((static_cast<int64_t>(n) * g.group + ROWS - 1) / ROWS);
+  *pages = len <= 0 ? 0 : (min(len, g.max_len) + PAGE - 1) / PAGE;
+}
+// a lane's value, in scalar registers: what follows from it is worked out once per wave
+__device__ inline int64_t of_lane(int64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), lane);
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ inline int64_t sum_of_wave(int64_t x) {
+  for (int off = 1; off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
+  return of_lane(x, 0);
+}
+__device__ inline int splits_of(int pages, int split_pages) { return pages > split_pages ? (pages + split_pages - 1) / split_pages : 1; }
+template <int ROWS>
+__device__ inline Deal deal(const CachedArgs& g) {
+  const int lane = threadIdx.x & 63;
+  Deal d;
+  int tiles, pages, first_tiles = 0, first_pages = 0;
+  int64_t work = 0, whole = 0;
+  for (int s0 = 0; s0 < g.seqs.n; s0 += 64) {
+    deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
+    if (s0 == 0) { first_tiles = tiles; first_pages = pages; }
+    work += static_cast<int64_t>(tiles) * pages;
+    whole += tiles;
+  }
+  work = sum_of_wave(work) * g.kv_heads;
+  whole = sum_of_wave(whole) * g.kv_heads;
+  const int64_t resident = g.resident;
+  const int64_t ranges = 4 * whole <= resident ? resident - whole : max(4 * resident - whole, 2 * resident), each = (work + ranges - 1) / ranges;
+  d.split_pages = __builtin_amdgcn_readfirstlane(static_cast<int>(each > g.least_pages ? each : g.least_pages));
+  d.tiles = first_tiles;
+  d.pages = first_pages;
+  d.units = static_cast<int64_t>(d.tiles) * splits_of(d.pages, d.split_pages);
+  for (int s0 = 64; s0 < g.seqs.n; s0 += 64) {
+    deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
+    d.units += static_cast<int64_t>(tiles) * splits_of(pages, d.split_pages);
+  }
+  d.units = sum_of_wave(d.units) * g.kv_heads;
+  return d;
+}
+// Sequence of unit u, u's number within it and the slot of its first unit.  (u rises through tiles first, then splits, then heads: blocks that
+// run side by side read the same keys.)  With seq >= 0 the slot of that sequence is looked for instead.
+struct Found {
+  int seq, tiles, splits, at;
+  int each;                         // pages of a split
+  int64_t slot;
+};
+template <int ROWS>
+__device__ inline Found find_unit(const CachedArgs& g, const Deal& d, int64_t u, int seq) {
+  const int lane = threadIdx.x & 63;
+  Found f{-1, 0, 1, 0, 0, 0};
+  int64_t before = 0, slots = 0;
+  for (int s0 = 0; s0 < g.seqs.n; s0 += 64) {
+    int tiles = d.tiles, pages = d.pages;
+    if (s0) deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
+    const int splits = splits_of(pages, d.split_pages);
+    const int64_t mine = static_cast<int64_t>(tiles) * splits * g.kv_heads, mine_slots = splits > 1 ? mine : 0;
+    int64_t upto = mine, upto_slots = mine_slots;
+    for (int off = 1; off < 64; off <<= 1) {
+      const int64_t a = __shfl_up(upto, off, 64), b = __shfl_up(upto_slots, off, 64);
+      if (lane >= off) { upto += a; upto_slots += b; }
+    }
+    const uint64_t hit = __ballot(seq < 0 ? before + upto > u : s0 + lane == seq);
+    if (hit) {
+      const int l = __builtin_ctzll(hit);
+      f.seq = s0 + l;
+      f.tiles = __builtin_amdgcn_readlane(tiles, l);
+      f.splits = __builtin_amdgcn_readlane(splits, l);
+      f.each = (__builtin_amdgcn_readlane(pages, l) + f.splits - 1) / f.splits;
+      f.at = static_cast<int>(u - before - of_lane(upto - mine, l));
+      f.slot = slots + of_lane(upto_slots - mine_slots, l);
+      return f;
+    }
+    before += of_lane(upto, 63);
+    slots += of_lane(upto_slots, 63);
+  }
+  return f;
+}
+
+// 128 rows a tile, head_dim 64, 72 or 128 (attn_cached_tile.hip).
+void launch_attention_cached_tile(const CachedArgs& g, int head_dim, unsigned blocks, hipStream_t st);
+
+}  // namespace speca

@@ -12,14 +12,11 @@
 #include <cmath>
 
 #include "gemm.h"
-#include "attn_lane.h"
-#include "operators.h"
+#include "attn_cached.h"
 
 namespace speca {
 
 namespace {
-
-constexpr int PAGE = SPECA_KV_PAGE;
 
 typedef uint32_t u32x4_at8 __attribute__((ext_vector_type(4), aligned(8)));       // head size 72: rows of 72 bytes
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -29,29 +26,8 @@ union Frag {
   bf16x8 v;
 };
 
-// four e4m3 bytes x a power of two -> four bf16
-__device__ inline void widen(uint32_t b, float scale, uint32_t* out) {
-  const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
-  out[0] = *reinterpret_cast<const uint32_t*>(&lo);
-  out[1] = *reinterpret_cast<const uint32_t*>(&hi);
-}
-struct Args {
-  const uint8_t *k, *v;
-  const float *k_scale, *v_scale;
-  const uint16_t* q;
-  uint16_t* out;
-  int64_t ldq, ldo;
-  Packed seqs;
-  const int32_t *lens, *table;
-  float *part, *stats;              // of splits: O [block][16 NQ][HD], then maximum and sum [block][2][16 NQ]
-  int32_t table_ld, pages, kv_heads, group;
-  int32_t max_len, splits, split_pages;
-  int32_t causal, wide;             // wide: queries at whole 16 bytes, outputs at whole 8
-  float scale_log2e;
-};
-
 template <int HD, int NQ>
-__global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(const Args g) {
+__global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedArgs g) {
   constexpr int FULL = HD / 64, REM = HD % 64;
   constexpr int KS = 2 * FULL + (REM ? 1 : 0);     // steps of 32 columns
   constexpr int DT = (HD + 15) / 16;
@@ -62,13 +38,19 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
-  const int split = blockIdx.x % g.splits, rest = blockIdx.x / g.splits, head = rest % g.kv_heads, tile = rest / g.kv_heads;
-  const int seq = packed_find(g.seqs, tile, g.group, ROWS, 0);
+  const Deal d = deal<ROWS>(g);
+  // Blocks b, b + 8, ... run on the same XCD: a round of the grid gives each XCD a run of units, which share keys where rows are many.
+  const int per_xcd = gridDim.x / 8;
+  for (int64_t round = 0;; ++round) {
+  const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+  if (round * gridDim.x >= d.units) break;
+  if (unit >= d.units) continue;
+  const Found f = find_unit<ROWS>(g, d, unit, -1);
+  if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;        // (offsets that overlap: there is no room for their sums)
+  const int tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits, seq = f.seq;
   int start, n;
   packed_rows(g.seqs, seq, &start, &n);
-  const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS;
-  const int64_t rows = static_cast<int64_t>(n) * g.group;
-  if (r0 < 0 || r0 >= rows) return;
+  const int64_t r0 = static_cast<int64_t>(tile) * ROWS, rows = static_cast<int64_t>(n) * g.group;
   int len = g.lens[seq];
   len = len < 0 ? 0 : min(len, g.max_len);
 
@@ -83,7 +65,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
   }
   const int last_tok = static_cast<int>((min(r0 + ROWS, rows) - 1) / g.group), first_tok = static_cast<int>(r0 / g.group);
   const int most = g.causal ? max(0, len - n + last_tok + 1) : len, least = g.causal ? max(0, len - n + first_tok + 1) : len;
-  const int begin = split * g.split_pages, end = min(begin + g.split_pages, (most + PAGE - 1) / PAGE);
+  const int begin = split * f.each, end = min(begin + f.each, (most + PAGE - 1) / PAGE);
 
   bf16x8 qf[KS][NQ];
 #pragma unroll
@@ -147,17 +129,37 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
       vr[dt] = *reinterpret_cast<const u32x4*>(p + (d < HD ? d : HD - 1) * PAGE);        // beyond the head: any, never stored
     }
   };
-  // number of page j of the sequence, or -1: not held
-  auto page_of = [&](int j) {
-    const int p = j < g.table_ld ? table[j] : -1;
-    return __builtin_amdgcn_readfirstlane(p < 0 || p >= g.pages ? -1 : p);
+  // Numbers of the wave's next 64 pages, one a lane; those that are not held are passed over.  (Lengths are bounded by the table's row.)
+  int ids = -1, j = begin + wave, ids_from = j;
+  auto fetch_ids = [&] {
+    ids_from = j;
+    const int at = j + 4 * lane;
+    ids = at < end ? table[at] : -1;
+    if (ids >= g.pages) ids = -1;
   };
-
-  for (int j = begin + wave; j < end; j += 4) {
-    const int page = page_of(j);
-    if (page < 0) continue;
+  auto page_at = [&] {                             // of j, or of the first one held behind it
+    for (;;) {
+      if (j >= end) return -1;
+      if (j - ids_from >= 256) fetch_ids();
+      const uint64_t held = __ballot(ids >= 0) >> ((j - ids_from) >> 2);
+      if (held) {
+        j += 4 * __builtin_ctzll(held);
+        return __builtin_amdgcn_readlane(ids, (j - ids_from) >> 2);
+      }
+      j = ids_from + 256;
+    }
+  };
+  fetch_ids();
+  int page = page_at();
+  if (page >= 0) {
     load_k(page);
     load_v(page);
+  }
+  while (page >= 0) {
+    const int here = j;
+    j += 4;
+    const int next = page_at();
+    const float vscale = vs;
     floatx4 s[4][NQ];
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
@@ -175,7 +177,8 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
         for (int i = 0; i < NQ; ++i) s[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[t][i], t ? s[m][i] : floatx4{}, 0, 0, 0);
       }
     }
-    const bool edge = (j + 1) * PAGE > least;
+    if (next >= 0) load_k(next);                   // its operands are in registers by now
+    const bool edge = (here + 1) * PAGE > least;
     bool odd = false;                              // the page holds a NaN that some row does not see
     if (edge) {
 #pragma unroll
@@ -184,11 +187,11 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
         for (int m = 0; m < 4; ++m)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (j * PAGE + 16 * m + 4 * g4 + e >= lim[i]) s[m][i][e] = -INFINITY;
+            if (here * PAGE + 16 * m + 4 * g4 + e >= lim[i]) s[m][i][e] = -INFINITY;
       }
 #pragma unroll
       for (int m = 0; m < 4; ++m) {                // bytes past the last token: whatever they are, 0 now
-        const int c = len - (j * PAGE + 16 * m + 4 * g4);
+        const int c = len - (here * PAGE + 16 * m + 4 * g4);
         const uint32_t keep = c >= 4 ? ~0u : c <= 0 ? 0u : (1u << (8 * c)) - 1u;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
@@ -212,7 +215,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
       corr[i] = fast_exp2(mref[i] * g.scale_log2e - moff);
       moved |= mnew != mref[i];
       mref[i] = mnew;
-      seen[i] |= j * PAGE < lim[i];
+      seen[i] |= here * PAGE < lim[i];
       float sum = 0.0f;
 #pragma unroll
       for (int m = 0; m < 4; ++m)
@@ -251,7 +254,7 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
             Frag b;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const int key = j * PAGE + 16 * (2 * u + e / 2) + 4 * g4 + 2 * (e % 2);
+              const int key = here * PAGE + 16 * (2 * u + e / 2) + 4 * g4 + 2 * (e % 2);
               b.u[e] = (key < lim[i] ? 0x3F80u : 0u) | (key + 1 < lim[i] ? 0x3F800000u : 0u);
             }
             hit[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, u ? hit[i] : floatx4{}, 0, 0, 0);
@@ -281,11 +284,13 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         Frag f;
-        widen(vr[dt][2 * u], vs, f.u);
-        widen(vr[dt][2 * u + 1], vs, f.u + 2);
+        widen(vr[dt][2 * u], vscale, f.u);
+        widen(vr[dt][2 * u + 1], vscale, f.u + 2);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) o[dt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, pf[u][i], o[dt][i], 0, 0, 0);
       }
+    if (next >= 0) load_v(next);
+    page = next;
   }
 
   // together: everything relative to the largest maximum of the four waves; wave w sums the dimensions of tiles w, w + 4, ...
@@ -315,12 +320,12 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
     for (int dt = 0; dt < DT; ++dt) merge[wave][dt * NQ + i][lane] = o[dt][i] * f;
   }
   __syncthreads();
-  const int64_t block = blockIdx.x;
-  if (g.splits > 1 && wave == 0 && g4 == 0) {
+  const int64_t slot = f.slot + f.at;
+  if (f.splits > 1 && wave == 0 && g4 == 0) {
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
-      g.stats[block * 2 * ROWS + i * 16 + l16] = top[i];
-      g.stats[block * 2 * ROWS + ROWS + i * 16 + l16] = total[i];
+      g.stats[slot * 2 * ROWS + i * 16 + l16] = top[i];
+      g.stats[slot * 2 * ROWS + ROWS + i * 16 + l16] = total[i];
     }
   }
 #pragma unroll
@@ -331,8 +336,8 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       const floatx4 v = (merge[0][dt * NQ + i][lane] + merge[1][dt * NQ + i][lane]) + (merge[2][dt * NQ + i][lane] + merge[3][dt * NQ + i][lane]);
-      if (g.splits > 1) {
-        *reinterpret_cast<floatx4*>(g.part + (block * ROWS + i * 16 + l16) * HD + d) = v;
+      if (f.splits > 1) {
+        *reinterpret_cast<floatx4*>(g.part + (slot * ROWS + i * 16 + l16) * HD + d) = v;
       } else if (r0 + i * 16 + l16 < rows) {
         uint16_t* op = g.out + (static_cast<int64_t>(start) + tok[i]) * g.ldo + (static_cast<int64_t>(head) * g.group + sub[i]) * HD + d;
         const float inv = total[i] == 0.0f ? 0.0f : 1.0f / total[i];
@@ -342,79 +347,110 @@ __global__ __launch_bounds__(256, NQ == 4 ? 1 : 2) void attention_cached_kernel(
       }
     }
   }
-}
-
-// Joins the splits of 16 NQ rows, in their order.
-template <int HD, int NQ>
-__global__ __launch_bounds__(256) void attention_cached_join_kernel(const Args g) {
-  constexpr int ROWS = 16 * NQ;
-  const int head = blockIdx.x % g.kv_heads, tile = blockIdx.x / g.kv_heads;
-  const int seq = packed_find(g.seqs, tile, g.group, ROWS, 0);
-  int start, n;
-  packed_rows(g.seqs, seq, &start, &n);
-  const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS;
-  const int64_t rows = static_cast<int64_t>(n) * g.group;
-  if (r0 < 0 || r0 >= rows) return;
-  const int64_t first = static_cast<int64_t>(blockIdx.x) * g.splits;
-  for (int at = threadIdx.x; at < ROWS * (HD / 4); at += 256) {
-    const int r = at / (HD / 4), d = (at - r * (HD / 4)) * 4;
-    if (r0 + r >= rows) break;
-    float top = -INFINITY;
-    for (int s = 0; s < g.splits; ++s) top = fmaxf(top, g.stats[(first + s) * 2 * ROWS + r]);
-    const float off = top == -INFINITY ? 0.0f : top * g.scale_log2e;
-    float total = 0.0f;
-    floatx4 v = {};
-    for (int s = 0; s < g.splits; ++s) {
-      const float m = g.stats[(first + s) * 2 * ROWS + r], l = g.stats[(first + s) * 2 * ROWS + ROWS + r];
-      if (m == -INFINITY && top != -INFINITY) continue;
-      const float f = m == -INFINITY ? 1.0f : fast_exp2(m * g.scale_log2e - off);
-      total += l * f;
-      v += *reinterpret_cast<const floatx4*>(g.part + ((first + s) * ROWS + r) * HD + d) * f;
-    }
-    const int tok = static_cast<int>((r0 + r) / g.group), sub = static_cast<int>(r0 + r - static_cast<int64_t>(tok) * g.group);
-    uint16_t* op = g.out + (static_cast<int64_t>(start) + tok) * g.ldo + (static_cast<int64_t>(head) * g.group + sub) * HD + d;
-    const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-    const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
-    if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
-    else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+  __syncthreads();                                 // the next unit writes the statistics again
   }
 }
 
+// Joins the splits of four rows of a tile of ROWS: each wave sums every fourth split, in their order, then the waves' sums are added.  Lane: four
+// columns of one of two rows at a time.
+template <int HD, int ROWS>
+__global__ __launch_bounds__(256) void attention_cached_join_kernel(const CachedArgs g) {
+  constexpr int C = HD / 4;                        // lanes of a row
+  static_assert(C <= 32, "two rows a wave");
+  __shared__ float tops[4][4];
+  __shared__ __align__(16) floatx4 sums[4][4][C];
+  __shared__ float totals[4][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int quad = blockIdx.x % (ROWS / 4), rest = blockIdx.x / (ROWS / 4), head = rest % g.kv_heads, tile = rest / g.kv_heads;
+  const int seq = packed_find(g.seqs, tile, g.group, ROWS, 0);
+  int start, n;
+  packed_rows(g.seqs, seq, &start, &n);
+  const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS, rows = static_cast<int64_t>(n) * g.group;
+  if (r0 < 0 || r0 + quad * 4 >= rows) return;
+  const Deal d = deal<ROWS>(g);
+  const Found f = find_unit<ROWS>(g, d, 0, seq);
+  if (f.splits == 1 || f.slot + static_cast<int64_t>(f.tiles) * f.splits * g.kv_heads > g.slots) return;
+  const int64_t first = f.slot + static_cast<int64_t>(head) * f.splits * f.tiles + r0 / ROWS;
+  auto stat = [&](int s, int which, int r) { return g.stats[((first + static_cast<int64_t>(s) * f.tiles) * 2 + which) * ROWS + quad * 4 + r]; };
+
+  float top = -INFINITY;                           // of row lane % 4, over the splits of this lane, then of all
+  for (int s = tid >> 2; s < f.splits; s += 64) top = fmaxf(top, stat(s, 0, tid & 3));
+  for (int off = 4; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+  if (lane < 4) tops[wave][lane] = top;
+  __syncthreads();
+  const int col = lane & 31;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int r = 2 * half + (lane >> 5);
+    const float m = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+    const float off = m == -INFINITY ? 0.0f : m * g.scale_log2e;
+    float total = 0.0f;
+    floatx4 v = {};
+#pragma unroll 4
+    for (int s = wave; s < f.splits; s += 4) {
+      const float ms = stat(s, 0, r), l = stat(s, 1, r);
+      const floatx4 x = *reinterpret_cast<const floatx4*>(g.part + ((first + static_cast<int64_t>(s) * f.tiles) * ROWS + quad * 4 + r) * HD + 4 * (col < C ? col : 0));
+      // a split without a finite score has weight 0, unless all are so: then NaN where keys were seen, 0 elsewhere
+      const float w = ms == -INFINITY ? (m == -INFINITY ? 1.0f : 0.0f) : fast_exp2(ms * g.scale_log2e - off);
+      total += ms == -INFINITY && w == 0.0f ? 0.0f : l * w;
+      v += x * w;
+    }
+    if (col < C) sums[wave][r][col] = v;
+    if (col == 0) totals[wave][r] = total;
+  }
+  __syncthreads();
+  if (tid >= 4 * C) return;
+  const int r = tid / C, c = tid - r * C;
+  if (r0 + quad * 4 + r >= rows) return;
+  const floatx4 v = (sums[0][r][c] + sums[1][r][c]) + (sums[2][r][c] + sums[3][r][c]);
+  const float total = (totals[0][r] + totals[1][r]) + (totals[2][r] + totals[3][r]);
+  const int64_t row = r0 + quad * 4 + r;
+  const int tok = static_cast<int>(row / g.group), sub = static_cast<int>(row - static_cast<int64_t>(tok) * g.group);
+  uint16_t* op = g.out + (static_cast<int64_t>(start) + tok) * g.ldo + (static_cast<int64_t>(head) * g.group + sub) * HD + 4 * c;
+  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+  const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
+  if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
+  else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+}
+
 struct Plan {
-  int nq, splits, split_pages;
-  int64_t tiles, blocks;
-  size_t part_bytes, bytes;
+  int rows;                         // of a tile
+  int resident, least_pages;
+  int64_t tiles, units;             // at most
+  int64_t slots;                    // at most; 0: no sequence is long enough to be split
+  int64_t part_bytes, bytes;
 };
 Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
   Plan p{};
   const int group = heads / kv_heads;
-  const int64_t rows = static_cast<int64_t>(total) * group, mean = (rows + n_seqs - 1) / n_seqs;
-  p.nq = mean <= 16 ? 1 : mean <= 32 ? 2 : 4;
-  p.tiles = rows / (16 * p.nq) + n_seqs;
-  const int pages = (max_len + PAGE - 1) / PAGE;
-  // as many blocks as give every unit four, each of at least 8 pages
-  const int64_t busy = std::max<int64_t>(1, std::min<int64_t>(p.tiles, n_seqs * ((mean + 16 * p.nq - 1) / (16 * p.nq)))) * kv_heads;
-  p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((4 * 256 + busy - 1) / busy, pages / 8)));
-  p.split_pages = std::max(1, (pages + p.splits - 1) / p.splits);
-  p.splits = std::max(1, (pages + p.split_pages - 1) / p.split_pages);
-  p.blocks = p.tiles * kv_heads * p.splits;
-  if (p.splits > 1) {
-    p.part_bytes = static_cast<size_t>(p.blocks) * 16 * p.nq * head_dim * sizeof(float);
-    p.bytes = p.part_bytes + static_cast<size_t>(p.blocks) * 2 * 16 * p.nq * sizeof(float);
+  const int64_t rows = static_cast<int64_t>(total) * group, mean = (rows + n_seqs - 1) / n_seqs, pages = (static_cast<int64_t>(max_len) + PAGE - 1) / PAGE;
+  p.rows = mean <= 16 ? 16 : mean <= 32 || head_dim < 64 ? 32 : 128;
+  p.tiles = rows / p.rows + n_seqs;
+  p.resident = 2 * compute_units();
+  p.least_pages = 8;
+  const int64_t whole = p.tiles * kv_heads;
+  if (pages > p.least_pages) {
+    p.slots = std::min<int64_t>(4 * p.resident, whole * ((pages + p.least_pages - 1) / p.least_pages));
+    p.part_bytes = p.slots * p.rows * head_dim * static_cast<int64_t>(sizeof(float));
+    p.bytes = p.part_bytes + p.slots * 2 * p.rows * static_cast<int64_t>(sizeof(float));
   }
+  p.units = whole + p.slots;
   return p;
 }
 
-template <int HD, int NQ>
-void launch_nq(const Args& g, const Plan& p, hipStream_t st) {
-  attention_cached_kernel<HD, NQ><<<static_cast<unsigned>(p.blocks), 256, 0, st>>>(g);
-  if (p.splits > 1) attention_cached_join_kernel<HD, NQ><<<static_cast<unsigned>(p.tiles * g.kv_heads), 256, 0, st>>>(g);
-}
 template <int HD>
-void launch_hd(const Args& g, const Plan& p, hipStream_t st) {
-  if (p.nq == 1) launch_nq<HD, 1>(g, p, st);
-  else if (p.nq == 2) launch_nq<HD, 2>(g, p, st);
-  else launch_nq<HD, 4>(g, p, st);
+void launch_hd(const CachedArgs& g, const Plan& p, hipStream_t st) {
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(p.units, p.resident)), joins = static_cast<unsigned>(p.tiles * g.kv_heads * (p.rows / 4));
+  if (p.rows == 16) {
+    attention_cached_kernel<HD, 1><<<blocks, 256, 0, st>>>(g);
+    if (p.slots) attention_cached_join_kernel<HD, 16><<<joins, 256, 0, st>>>(g);
+  } else if (p.rows == 32) {
+    attention_cached_kernel<HD, 2><<<blocks, 256, 0, st>>>(g);
+    if (p.slots) attention_cached_join_kernel<HD, 32><<<joins, 256, 0, st>>>(g);
+  } else if constexpr (HD >= 64) {
+    launch_attention_cached_tile(g, HD, blocks, st);
+    if (p.slots) attention_cached_join_kernel<HD, 128><<<joins, 256, 0, st>>>(g);
+  }
 }
 
 bool sizes_ok(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
@@ -426,7 +462,7 @@ bool sizes_ok(int n_seqs, int total, int max_len, int heads, int kv_heads, int h
 
 int64_t attention_cached_workspace(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
   if (!sizes_ok(n_seqs, total, max_len, heads, kv_heads, head_dim)) return -1;
-  return total == 0 ? 0 : static_cast<int64_t>(plan_of(n_seqs, total, max_len, heads, kv_heads, head_dim).bytes);
+  return total == 0 ? 0 : plan_of(n_seqs, total, max_len, heads, kv_heads, head_dim).bytes;
 }
 
 Error launch_attention_cached(int dtype, const speca_kv_cache& c, const speca_kv_table& t, const CachedAttention& a, void* workspace,
@@ -447,10 +483,10 @@ Error launch_attention_cached(int dtype, const speca_kv_cache& c, const speca_kv
   if (!(a.scale >= 0.0f) || !std::isfinite(a.scale)) SPECA_FAIL(SPECA_EINVAL, "%s: scale = %g", who, a.scale);
   if (a.seqs.total == 0) return ok();
   const Plan p = plan_of(a.seqs.n, a.seqs.total, a.max_len, a.heads, c.kv_heads, c.head_dim);
-  if (p.blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "%s: %d tokens of %d heads are too many for one call", who, a.seqs.total, a.heads);
-  if (p.bytes && (!workspace || workspace_bytes < static_cast<int64_t>(p.bytes) || reinterpret_cast<uintptr_t>(workspace) % 16))
-    SPECA_FAIL(SPECA_EINVAL, "%s: a workspace of %zu bytes, 16-byte aligned, is needed (given: %lld)", who, p.bytes, static_cast<long long>(workspace ? workspace_bytes : 0));
-  Args g;
+  if (p.tiles * c.kv_heads * (p.rows / 4) > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "%s: %d tokens of %d heads are too many for one call", who, a.seqs.total, a.heads);
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16))
+    SPECA_FAIL(SPECA_EINVAL, "%s: a workspace of %lld bytes, 16-byte aligned, is needed (given: %lld)", who, static_cast<long long>(p.bytes), static_cast<long long>(workspace ? workspace_bytes : 0));
+  CachedArgs g;
   g.k = static_cast<const uint8_t*>(c.k); g.v = static_cast<const uint8_t*>(c.v);
   g.k_scale = c.k_scale; g.v_scale = c.v_scale;
   g.q = static_cast<const uint16_t*>(a.q); g.out = static_cast<uint16_t*>(a.out);
@@ -461,7 +497,7 @@ Error launch_attention_cached(int dtype, const speca_kv_cache& c, const speca_kv
   g.stats = p.bytes ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes) : nullptr;
   g.table_ld = t.ld; g.pages = c.pages; g.kv_heads = c.kv_heads; g.group = a.heads / c.kv_heads;
   g.max_len = static_cast<int>(std::min<int64_t>(a.max_len, static_cast<int64_t>(t.ld) * PAGE));
-  g.splits = p.splits; g.split_pages = p.split_pages;
+  g.resident = p.resident; g.least_pages = p.least_pages; g.slots = static_cast<int32_t>(p.slots);
   g.causal = a.causal;
   g.wide = at % 16 == 0 && a.ldq % 8 == 0 && to % 8 == 0 && a.ldo % 4 == 0;
   g.scale_log2e = 1.4426950408889634f * (a.scale == 0.0f ? 1.0f / std::sqrt(static_cast<float>(c.head_dim)) : a.scale);

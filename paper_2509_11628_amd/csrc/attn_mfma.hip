@@ -477,6 +477,8 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
     if constexpr (!NEXT && MODE == CAUSAL) {
       union Words { bf16x8 v; uint32_t u[4]; };
       uint32_t any = 0;
+      int from = buf;                       // read again further down, rather than kept from here
+      asm volatile("" : "+s"(from));
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         Words x;
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
           Words x, y;
-          x.v = value_frag(buf, i / DT, i % DT);
+          x.v = value_frag(from, i / DT, i % DT);
 #pragma unroll
           for (int j = 0; j < 4; ++j) y.u[j] = without_odd(x.u[j]);
 #pragma unroll
