@@ -30,10 +30,11 @@ struct CachedArgs {
 };
 
 // How the work is dealt.  The host knows no lengths, so every wave works it out from the lists on the device, 64 sequences at a time.  A unit is
-// one row tile of one key head over one split of its sequence's range of pages.  With `whole` units if nothing is split and W pages to visit in
-// all, ranges longer than split_pages = W / E are split evenly, which makes at most min(W / split_pages + whole, 2 W / split_pages) units of split ranges:
-//   whole <= resident / 4:  E = resident - whole             one round of the blocks that fit on the chip, none idle for long
-//   otherwise:              E = max(4 resident - whole, 2 resident)  four rounds, so that the last one, which is not full, costs little
+// one row tile of one key head over one split of its sequence's range of pages; ranges longer than split_pages are split evenly.  With `whole` units
+// if nothing is split and W pages to visit in all, split_pages = W / E makes at most min(E + whole, 2 E) units of split ranges.
+//   whole <= resident / 4:  E = resident - whole: one round of the blocks that fit on the chip
+//   otherwise:              E = R resident - whole for the R of 1 to 4 whose rounds x (longest unit + 4 pages that it takes to begin and end one) are
+//                           fewest (E = 2 resident where no R has room)
 // and never more than 4 resident of them, which is what the workspace has room for.
 struct Deal {
   int tiles, pages;                 // of the lane's sequence in the first 64
@@ -60,31 +61,58 @@ __device__ inline int64_t sum_of_wave(int64_t x) {
   return of_lane(x, 0);
 }
 __device__ inline int splits_of(int pages, int split_pages) { return pages > split_pages ? (pages + split_pages - 1) / split_pages : 1; }
+__device__ inline int max_of_wave(int x) {
+  for (int off = 1; off < 64; off <<= 1) x = max(x, __shfl_xor(x, off, 64));
+  return __builtin_amdgcn_readlane(x, 0);
+}
 template <int ROWS>
 __device__ inline Deal deal(const CachedArgs& g) {
   const int lane = threadIdx.x & 63;
   Deal d;
-  int tiles, pages, first_tiles = 0, first_pages = 0;
-  int64_t work = 0, whole = 0;
-  for (int s0 = 0; s0 < g.seqs.n; s0 += 64) {
+  deal_sequence<ROWS>(g, lane, &d.tiles, &d.pages);
+  int64_t work = static_cast<int64_t>(d.tiles) * d.pages, whole = d.tiles;
+  int tiles, pages;
+  for (int s0 = 64; s0 < g.seqs.n; s0 += 64) {
     deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
-    if (s0 == 0) { first_tiles = tiles; first_pages = pages; }
     work += static_cast<int64_t>(tiles) * pages;
     whole += tiles;
   }
   work = sum_of_wave(work) * g.kv_heads;
   whole = sum_of_wave(whole) * g.kv_heads;
+  auto pages_for = [&](int64_t ranges) { return static_cast<int>(max(static_cast<int64_t>(g.least_pages), (work + ranges - 1) / ranges)); };
+  // units of all sequences, and pages of the longest
+  auto count = [&](int split_pages, int64_t* units, int* longest) {
+    int splits = splits_of(d.pages, split_pages), most = d.tiles ? (d.pages + splits - 1) / splits : 0;
+    int64_t sum = static_cast<int64_t>(d.tiles) * splits;
+    for (int s0 = 64; s0 < g.seqs.n; s0 += 64) {
+      deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
+      splits = splits_of(pages, split_pages);
+      sum += static_cast<int64_t>(tiles) * splits;
+      if (tiles) most = max(most, (pages + splits - 1) / splits);
+    }
+    *units = sum_of_wave(sum) * g.kv_heads;
+    if (longest) *longest = max_of_wave(most);
+  };
   const int64_t resident = g.resident;
-  const int64_t ranges = 4 * whole <= resident ? resident - whole : max(4 * resident - whole, 2 * resident), each = (work + ranges - 1) / ranges;
-  d.split_pages = __builtin_amdgcn_readfirstlane(static_cast<int>(each > g.least_pages ? each : g.least_pages));
-  d.tiles = first_tiles;
-  d.pages = first_pages;
-  d.units = static_cast<int64_t>(d.tiles) * splits_of(d.pages, d.split_pages);
-  for (int s0 = 64; s0 < g.seqs.n; s0 += 64) {
-    deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
-    d.units += static_cast<int64_t>(tiles) * splits_of(pages, d.split_pages);
+  if (4 * whole <= resident) {
+    d.split_pages = pages_for(resident - whole);
+    count(d.split_pages, &d.units, nullptr);
+    return d;
   }
-  d.units = sum_of_wave(d.units) * g.kv_heads;
+  int64_t best = -1;
+  for (int rounds = 1; rounds <= 4 || best < 0; ++rounds) {
+    const int64_t ranges = rounds <= 4 ? rounds * resident - whole : 2 * resident;
+    if (ranges <= 0) continue;
+    const int split_pages = pages_for(ranges);
+    int64_t units;
+    int longest;
+    count(split_pages, &units, &longest);
+    const int64_t cost = (units + resident - 1) / resident * (longest + 4);
+    if (best >= 0 && cost >= best) continue;
+    best = cost;
+    d.split_pages = split_pages;
+    d.units = units;
+  }
   return d;
 }
 // Sequence of unit u, u's number within it and the slot of its first unit.  (u rises through tiles first, then splits, then heads: blocks that

@@ -351,26 +351,27 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
   }
 }
 
-// Joins the splits of four rows of a tile of ROWS: each wave sums every fourth split, in their order, then the waves' sums are added.  Lane: four
-// columns of one of two rows at a time.
+// Joins the splits of the rows of a tile of ROWS, four rows at a time, `quads` times per block: each wave sums every fourth split, in their order,
+// then the waves' sums are added.  Lane: four columns of rows lane / 32 and 2 + lane / 32.
 template <int HD, int ROWS>
-__global__ __launch_bounds__(256) void attention_cached_join_kernel(const CachedArgs g) {
+__global__ __launch_bounds__(256) void attention_cached_join_kernel(const CachedArgs g, int quads) {
   constexpr int C = HD / 4;                        // lanes of a row
   static_assert(C <= 32, "two rows a wave");
   __shared__ float tops[4][4];
   __shared__ __align__(16) floatx4 sums[4][4][C];
   __shared__ float totals[4][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int quad = blockIdx.x % (ROWS / 4), rest = blockIdx.x / (ROWS / 4), head = rest % g.kv_heads, tile = rest / g.kv_heads;
+  const int parts = ROWS / 4 / quads, part = blockIdx.x % parts, rest = blockIdx.x / parts, head = rest % g.kv_heads, tile = rest / g.kv_heads;
   const int seq = packed_find(g.seqs, tile, g.group, ROWS, 0);
   int start, n;
   packed_rows(g.seqs, seq, &start, &n);
   const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS, rows = static_cast<int64_t>(n) * g.group;
-  if (r0 < 0 || r0 + quad * 4 >= rows) return;
+  if (r0 < 0 || r0 + part * quads * 4 >= rows) return;
   const Deal d = deal<ROWS>(g);
   const Found f = find_unit<ROWS>(g, d, 0, seq);
   if (f.splits == 1 || f.slot + static_cast<int64_t>(f.tiles) * f.splits * g.kv_heads > g.slots) return;
   const int64_t first = f.slot + static_cast<int64_t>(head) * f.splits * f.tiles + r0 / ROWS;
+  for (int quad = part * quads; quad < (part + 1) * quads && r0 + quad * 4 < rows; ++quad) {
   auto stat = [&](int s, int which, int r) { return g.stats[((first + static_cast<int64_t>(s) * f.tiles) * 2 + which) * ROWS + quad * 4 + r]; };
 
   float top = -INFINITY;                           // of row lane % 4, over the splits of this lane, then of all
@@ -379,29 +380,35 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
   if (lane < 4) tops[wave][lane] = top;
   __syncthreads();
   const int col = lane & 31;
+  float m[2], off[2], total[2] = {};
+  floatx4 v[2] = {};
 #pragma unroll
   for (int half = 0; half < 2; ++half) {
     const int r = 2 * half + (lane >> 5);
-    const float m = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
-    const float off = m == -INFINITY ? 0.0f : m * g.scale_log2e;
-    float total = 0.0f;
-    floatx4 v = {};
+    m[half] = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+    off[half] = m[half] == -INFINITY ? 0.0f : m[half] * g.scale_log2e;
+  }
 #pragma unroll 4
-    for (int s = wave; s < f.splits; s += 4) {
+  for (int s = wave; s < f.splits; s += 4)
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int r = 2 * half + (lane >> 5);
       const float ms = stat(s, 0, r), l = stat(s, 1, r);
       const floatx4 x = *reinterpret_cast<const floatx4*>(g.part + ((first + static_cast<int64_t>(s) * f.tiles) * ROWS + quad * 4 + r) * HD + 4 * (col < C ? col : 0));
       // a split without a finite score has weight 0, unless all are so: then NaN where keys were seen, 0 elsewhere
-      const float w = ms == -INFINITY ? (m == -INFINITY ? 1.0f : 0.0f) : fast_exp2(ms * g.scale_log2e - off);
-      total += ms == -INFINITY && w == 0.0f ? 0.0f : l * w;
-      v += x * w;
+      const float w = ms == -INFINITY ? (m[half] == -INFINITY ? 1.0f : 0.0f) : fast_exp2(ms * g.scale_log2e - off[half]);
+      total[half] += ms == -INFINITY && w == 0.0f ? 0.0f : l * w;
+      v[half] += x * w;
     }
-    if (col < C) sums[wave][r][col] = v;
-    if (col == 0) totals[wave][r] = total;
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    const int r = 2 * half + (lane >> 5);
+    if (col < C) sums[wave][r][col] = v[half];
+    if (col == 0) totals[wave][r] = total[half];
   }
   __syncthreads();
-  if (tid >= 4 * C) return;
   const int r = tid / C, c = tid - r * C;
-  if (r0 + quad * 4 + r >= rows) return;
+  if (tid < 4 * C && r0 + quad * 4 + r < rows) {
   const floatx4 v = (sums[0][r][c] + sums[1][r][c]) + (sums[2][r][c] + sums[3][r][c]);
   const float total = (totals[0][r] + totals[1][r]) + (totals[2][r] + totals[3][r]);
   const int64_t row = r0 + quad * 4 + r;
@@ -411,6 +418,9 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
   const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
   if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
   else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+  }
+  __syncthreads();
+  }
 }
 
 struct Plan {
@@ -438,18 +448,26 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   return p;
 }
 
+template <int HD, int ROWS>
+void launch_join(const CachedArgs& g, const Plan& p, hipStream_t st) {
+  if (!p.slots) return;
+  // a block per four rows while that leaves the chip room, else one per 32
+  const int64_t quads = p.tiles * g.kv_heads * (ROWS / 4);
+  const int each = quads > 8 * p.resident ? (ROWS / 4 < 8 ? ROWS / 4 : 8) : 1;
+  attention_cached_join_kernel<HD, ROWS><<<static_cast<unsigned>(quads / each), 256, 0, st>>>(g, each);
+}
 template <int HD>
 void launch_hd(const CachedArgs& g, const Plan& p, hipStream_t st) {
-  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(p.units, p.resident)), joins = static_cast<unsigned>(p.tiles * g.kv_heads * (p.rows / 4));
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(p.units, p.resident));
   if (p.rows == 16) {
     attention_cached_kernel<HD, 1><<<blocks, 256, 0, st>>>(g);
-    if (p.slots) attention_cached_join_kernel<HD, 16><<<joins, 256, 0, st>>>(g);
+    launch_join<HD, 16>(g, p, st);
   } else if (p.rows == 32) {
     attention_cached_kernel<HD, 2><<<blocks, 256, 0, st>>>(g);
-    if (p.slots) attention_cached_join_kernel<HD, 32><<<joins, 256, 0, st>>>(g);
+    launch_join<HD, 32>(g, p, st);
   } else if constexpr (HD >= 64) {
     launch_attention_cached_tile(g, HD, blocks, st);
-    if (p.slots) attention_cached_join_kernel<HD, 128><<<joins, 256, 0, st>>>(g);
+    launch_join<HD, 128>(g, p, st);
   }
 }
 

@@ -29,6 +29,13 @@ __device__ inline int key_chunk(int c, int r) {
   return HD == 128 ? c ^ (r & 15) : HD == 64 ? c ^ (r & 7) ^ ((r >> 3) & 1) : c;
 }
 
+// Place of dimension l of lane group g among the 64 chunks of a value fragment: the 16 lanes {0-3, 12-15, 20-27} and so on that a read of 16 bytes takes
+// at a time hit different banks, and so do 8 threads that write four groups of two dimensions.
+__device__ inline int value_place(int l, int g) { return g * 16 + (l ^ (2 * g)); }
+
+// a value that all lanes read, in a scalar register
+__device__ inline float scalar(const float* p) { return *reinterpret_cast<const __attribute__((address_space(4))) float*>(reinterpret_cast<uintptr_t>(p)); }
+
 constexpr int ROWS = 128;
 
 template <int HD>
@@ -62,7 +69,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     if (4 * ks + 3 >= CH && 4 * ks + g4 >= CH) kc = zero;
     return *reinterpret_cast<const bf16x8*>(kc);
   };
-  auto value_frag = [&](int vb, int u, int dt) { return *reinterpret_cast<const bf16x8*>(Vs + vb * VTILE + ((u * DT + dt) * 64 + lane) * 8); };
+  const int vplace = value_place(l16, g4);
+  auto value_frag = [&](int vb, int u, int dt) { return *reinterpret_cast<const bf16x8*>(Vs + vb * VTILE + ((u * DT + dt) * 64 + vplace) * 8); };
 
   const Deal deal_ = deal<ROWS>(g);
   int number = 0;                             // of the block's unit
@@ -118,54 +126,46 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
       }
     }
 
-    // Pages of the unit, 64 numbers a time, one a lane; those that are not held are passed over.  (Lengths are bounded by the table's row.)
+    // Numbers of the unit's pages, 64 at a time, one a lane (lengths are bounded by the table's row).  One that is not held is worked on like the
+    // others, with some page's bytes, none of which any row sees.
     const int32_t* table = g.table + static_cast<int64_t>(f.seq) * g.table_ld;
-    int ids = -1, j = begin, ids_from = begin;
-    auto fetch_ids = [&] {
-      ids_from = j;
-      ids = j + lane < end ? table[j + lane] : -1;
-      if (ids >= g.pages) ids = -1;
+    const int tiles = end - begin;
+    int ids = -1;
+    int cache_pages = g.pages;
+    asm("" : "+s"(cache_pages));
+    auto number_of = [&](int t) {             // t rises
+      if ((t & 63) == 0) ids = t + lane < tiles ? table[begin + t + lane] : -1;
+      const int page = __builtin_amdgcn_readlane(ids, t & 63);
+      return page < 0 || page >= cache_pages ? -1 : page;
     };
-    auto page_at = [&] {                      // of j, or of the first one held behind it; -1: no more
-      for (;;) {
-        if (j >= end) return -1;
-        if (j - ids_from >= 64) fetch_ids();
-        const uint64_t held = __ballot(ids >= 0) >> (j - ids_from);
-        if (held) {
-          j += __builtin_ctzll(held);
-          return __builtin_amdgcn_readlane(ids, j - ids_from);
-        }
-        j = ids_from + 64;
-      }
-    };
-    int tiles = 0;                            // pages held
-    for (j = begin; j < end; j += 64) {
-      fetch_ids();
-      tiles += __popcll(__ballot(ids >= 0));
-    }
-    j = begin;
-    fetch_ids();
 
     // Staging: 8-byte units of the keys, 16-byte units of the values, linear in the page.
     typedef std::conditional_t<KW, u32x4, u32x2> KeyUnit;
     KeyUnit ka[KU];
     u32x4 va[VU];
     float kscale = 0.0f, vscale = 0.0f;
+    // Through buffer descriptors of a page: one register of offsets serves keys and values, and what lies beyond the page reads as zeros.
+    // (the addresses as values of their own: as parts of the arguments the compiler keeps and restores whole groups of them)
+    uint64_t k_at = reinterpret_cast<uint64_t>(g.k + static_cast<int64_t>(head) * (PAGE * HD)), v_at = reinterpret_cast<uint64_t>(g.v + static_cast<int64_t>(head) * (PAGE * HD));
+    uint64_t ks_at = reinterpret_cast<uint64_t>(g.k_scale + head), vs_at = reinterpret_cast<uint64_t>(g.v_scale + head);
+    uint32_t heads = g.kv_heads;
+    asm("" : "+s"(k_at), "+s"(v_at), "+s"(ks_at), "+s"(vs_at), "+s"(heads));
     auto load_k = [&](int page) {
-      const int64_t at = static_cast<int64_t>(page) * g.kv_heads + head;
-      const uint8_t* p = g.k + at * (PAGE * HD);
-      kscale = g.k_scale[at];
+      const uint64_t at = static_cast<uint64_t>(page < 0 ? 0 : page) * heads;
+      kscale = scalar(reinterpret_cast<const float*>(ks_at + at * 4));
+      const auto from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(k_at + at * (PAGE * HD)), 0, PAGE * HD, 0x00020000);
 #pragma unroll
-      for (int u = 0; u < KU; ++u)
-        if (KW || tid + 256 * u < 64 * CH) ka[u] = *reinterpret_cast<const KeyUnit*>(p + tid * sizeof(KeyUnit) + 256 * u * sizeof(KeyUnit));
+      for (int u = 0; u < KU; ++u) {
+        if constexpr (KW) ka[u] = __builtin_amdgcn_raw_buffer_load_b128(from, tid * 16, 4096 * u, 0);
+        else ka[u] = __builtin_amdgcn_raw_buffer_load_b64(from, tid * 8, 2048 * u, 0);
+      }
     };
     auto load_v = [&](int page) {
-      const int64_t at = static_cast<int64_t>(page) * g.kv_heads + head;
-      const uint8_t* p = g.v + at * (PAGE * HD);
-      vscale = g.v_scale[at];
+      const uint64_t at = static_cast<uint64_t>(page < 0 ? 0 : page) * heads;
+      vscale = scalar(reinterpret_cast<const float*>(vs_at + at * 4));
+      const auto from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(v_at + at * (PAGE * HD)), 0, PAGE * HD, 0x00020000);
 #pragma unroll
-      for (int u = 0; u < VU; ++u)
-        if (4 * HD % 256 == 0 || tid + 256 * u < 4 * HD) va[u] = *reinterpret_cast<const u32x4*>(p + tid * 16 + 4096 * u);
+      for (int u = 0; u < VU; ++u) va[u] = __builtin_amdgcn_raw_buffer_load_b128(from, tid * 16, 4096 * u, 0);
     };
     auto stage_k = [&](int buf, int u) {
       if constexpr (KW) {                     // rows CH / 2 units long: 512 / CH rows further with every u, which leaves the permutation as it is
@@ -173,9 +173,11 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           Frag x;
-          widen(ka[u][2 * h], kscale, x.u);
-          widen(ka[u][2 * h + 1], kscale, x.u + 2);
-          *reinterpret_cast<uint4*>(Ks + buf * KTILE + r * HD + (key_chunk<HD>(p + h, r) << 3) + u * (512 / CH) * HD) = x.q;
+          // every other four threads write their second chunk first: 8 threads then hit different banks
+          const bool turn = (tid & 4) != 0;
+          widen(turn ? ka[u][2 - 2 * h] : ka[u][2 * h], kscale, x.u);
+          widen(turn ? ka[u][3 - 2 * h] : ka[u][2 * h + 1], kscale, x.u + 2);
+          *reinterpret_cast<uint4*>(Ks + buf * KTILE + r * HD + (key_chunk<HD>(p + (turn ? 1 - h : h), r) << 3) + u * (512 / CH) * HD) = x.q;
         }
       } else {
         const int c = tid + 256 * u, r = static_cast<unsigned>(c) / CH, p = c - r * CH;
@@ -186,12 +188,14 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
         *reinterpret_cast<uint4*>(Ks + buf * KTILE + r * HD + (key_chunk<HD>(p, r) << 3)) = x.q;
       }
     };
-    // What is done once to the values of page `at` of the sequence where some row does not see all of it: bytes past the last token, whatever they
+    // Whether some row does not see all of page `at` of the sequence, which is page `page` of the cache.
+    auto is_edge = [&](int at, int page) { return (at + 1) * PAGE > least || page < 0; };
+    // What is done once to the values of such a page: bytes past the last token, whatever they
     // are, become 0, and so does a NaN, which must not meet the probability 0 of a row that does not see it.  The rows that do get it at the end.
-    auto edge_v = [&](int at) {
+    auto edge_v = [&](int at, int page) {
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
-        const int left = len - (at * PAGE + 4 * (tid & 3));
+        const int left = (page < 0 ? 0 : len) - (at * PAGE + 4 * (tid & 3));
         uint32_t any = 0;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
@@ -210,7 +214,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
       Frag x;
       widen(va[u][2 * half], vscale, x.u);
       widen(va[u][2 * half + 1], vscale, x.u + 2);
-      *reinterpret_cast<uint4*>(Vs + buf * VTILE + ((d >> 4) * 64 + grp * 16 + (d & 15)) * 8 + (half * DT + 4 * u) * 512) = x.q;
+      *reinterpret_cast<uint4*>(Vs + buf * VTILE + ((d >> 4) * 64 + value_place(d & 15, grp)) * 8 + (half * DT + 4 * u) * 512) = x.q;
     };
 
     floatx4 o[DT][2];
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
 #pragma unroll
       for (int i = from; i < to; ++i) tmax[(i >> 2) & 1] = fmaxf(tmax[(i >> 2) & 1], s[i >> 3][(i >> 2) & 1][i & 3]);
     };
-    auto reference = [&](int at) {
+    auto reference = [&](int at, int page) {
       moved = false;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -234,7 +238,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
         corr[i] = fast_exp2(mref[i] * scale_log2e - moff[i]);
         moved |= mnew != mref[i];
         mref[i] = mnew;
-        seen[i] |= at * PAGE < lim[i];
+        seen[i] |= page >= 0 && at * PAGE < lim[i];
       }
     };
     auto probabilities = [&](floatx4 (&s)[4][2], int from, int to) {
@@ -252,9 +256,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
                        cvt_pk_bf16(s[2 * u + 1][i][0], s[2 * u + 1][i][1]), cvt_pk_bf16(s[2 * u + 1][i][2], s[2 * u + 1][i][3]));
       return x.v;
     };
-    auto mask = [&](floatx4 (&s)[4][2], int at) {                    // keys that a row does not see
-      if ((at + 1) * PAGE <= least) return;
-      const int left[2] = {lim[0] - at * PAGE - 4 * g4, lim[1] - at * PAGE - 4 * g4};
+    auto mask = [&](floatx4 (&s)[4][2], int at, int page) {          // keys that a row does not see
+      const int left[2] = {page < 0 ? 0 : lim[0] - at * PAGE - 4 * g4, page < 0 ? 0 : lim[1] - at * PAGE - 4 * g4};
 #pragma unroll
       for (int i = 0; i < 32; ++i)
         if ((i >> 3) * 16 + (i & 3) >= left[(i >> 2) & 1]) s[i >> 3][(i >> 2) & 1][i & 3] = -INFINITY;
@@ -271,13 +274,14 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     SPECA_PIN();                                            \
   }
     constexpr int NS = 4 * KS, NV = 2 * DT, RA = 4, NP = 20;
-    // Tile in buffer `buf`, page `at` of the sequence, whose scores lie in sc with their reference known.  NEXT: its successor is page at1, whose
-    // keys lie in the other buffer and whose values are in va; the page behind that, whose keys are in ka, is page2, and page3 the one
-    // behind it.  (Where there is none, some page is loaded and staged, and not used.)
-    auto tile = [&](floatx4 (&sc)[4][2], floatx4 (&sn)[4][2], int buf, int at, int at1, int page2, int page3, auto next_tag) {
+    // Tile in buffer `buf`, whose scores lie in sc with their reference known.  NEXT: its successor is page at1 of the sequence, page1 of the cache,
+    // whose keys lie in the other buffer and whose values are in va; page2 is the one behind it, whose keys are in ka, and page3 the one behind
+    // that.  (Where there is none, some page is loaded and staged, and not used.)
+    auto tile = [&](floatx4 (&sc)[4][2], floatx4 (&sn)[4][2], int buf, int at1, int page1, int page2, int page3, auto next_tag) {
       constexpr bool NEXT = decltype(next_tag)::value;
       bf16x8 kf[NS], vf[NV], pf[2][2];
-      if (NEXT && (at1 + 1) * PAGE > least) edge_v(at1);
+      const bool edge = NEXT && is_edge(at1, page1);
+      if (edge) edge_v(at1, page1);
       constexpr int STEPS = KU + 2 * VU + 1;
       auto staging = [&](int i) {
         if constexpr (NEXT) {
@@ -329,7 +333,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
           if (i >= DT - 1 && i <= DT) pf[1][i - DT + 1] = pack(sc, 1, i - DT + 1);
           if (i < STEPS) staging(i);
           if constexpr (NEXT) {
-            if (i == DT) mask(sn, at1);
+            if (i == DT && edge) mask(sn, at1, page1);
           }
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
@@ -344,7 +348,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
         for (int i = NV; i < STEPS; ++i) staging(i);
 #pragma unroll
         for (int e = 0; e < 2; ++e) lrun[e] += psum[e];
-        if constexpr (NEXT) reference(at1);
+        if constexpr (NEXT) reference(at1, page1);
       } else {
 #pragma unroll
         for (int i = 0; i < STEPS; ++i) staging(i);
@@ -352,31 +356,24 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     };
 
     // Keys are loaded three pages ahead and staged two ahead, values one less.
-    int page0 = page_at(), at0 = j;
-    ++j;
-    int page1 = page0 < 0 ? -1 : page_at(), at1 = j;
-    ++j;
-    int page2 = page1 < 0 ? -1 : page_at(), at2 = j;
-    ++j;
     floatx4 sa[4][2], sb[4][2];
-    if (page0 >= 0) {
+    if (tiles > 0) {
+      int page0 = number_of(0), page1 = tiles > 1 ? number_of(1) : -1, page2 = tiles > 2 ? number_of(2) : -1;
       load_k(page0);
       load_v(page0);
       SPECA_TURN()                            // the unit before is through with LDS, and the zeros of the first are written
 #pragma unroll
       for (int u = 0; u < KU; ++u) stage_k(0, u);
-      if ((at0 + 1) * PAGE > least) edge_v(at0);
+      load_k(page1);
+      if (is_edge(begin, page0)) edge_v(begin, page0);
 #pragma unroll
       for (int u = 0; u < VU; ++u)
 #pragma unroll
         for (int h = 0; h < 2; ++h) stage_v(0, u, h);
-      if (page1 >= 0) {
-        load_k(page1);
-        load_v(page1);
+      load_v(page1);
 #pragma unroll
-        for (int u = 0; u < KU; ++u) stage_k(1, u);
-        load_k(page2 < 0 ? page1 : page2);
-      }
+      for (int u = 0; u < KU; ++u) stage_k(1, u);
+      load_k(page2);
       SPECA_TURN()
       if (active) {
 #pragma unroll
@@ -385,20 +382,18 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
 #pragma unroll
           for (int e = 0; e < 2; ++e) sa[i & 3][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[i >> 2][e], i < 4 ? floatx4{} : sa[i & 3][e], 0, 0, 0);
         }
-        mask(sa, at0);
+        if (is_edge(begin, page0)) mask(sa, begin, page0);
         tmax[0] = tmax[1] = -INFINITY;
         maximum(sa, 0, 32);
-        reference(at0);
+        reference(begin, page0);
       }
       // buffers alternate, and so do the two sets of scores
-#define SPECA_TILE(PAR, SC, SN)                                                        \
-  {                                                                                    \
-    const int page3 = page2 < 0 ? -1 : page_at(), at3 = j;                             \
-    ++j;                                                                               \
-    SPECA_TURN()                                                                       \
-    tile(SC, SN, PAR, at0, at1, page2 < 0 ? page1 : page2, page3 < 0 ? page1 : page3, std::true_type()); \
-    at0 = at1; at1 = at2; at2 = at3;                                                   \
-    page1 = page2; page2 = page3;                                                      \
+#define SPECA_TILE(PAR, SC, SN)                                                               \
+  {                                                                                           \
+    const int page3 = t + PAR + 3 < tiles ? number_of(t + PAR + 3) : -1;                      \
+    SPECA_TURN()                                                                              \
+    tile(SC, SN, PAR, begin + t + PAR + 1, page1, page2, page3, std::true_type());            \
+    page1 = page2; page2 = page3;                                                             \
   }
       int t = 0;
       for (; t + 2 < tiles; t += 2) {
@@ -415,7 +410,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
       }
 #undef SPECA_TILE
       SPECA_TURN()
-      tile(sa, sb, t & 1, at0, 0, -1, -1, std::false_type());
+      tile(sa, sb, t & 1, 0, 0, 0, 0, std::false_type());
       if (odd_unit == number) {               // (written ahead of the last turn)
         for (int at = max(begin, least / PAGE); at < end; ++at) {
           const int page = table[at];
