@@ -14,6 +14,11 @@ __device__ inline void widen(uint32_t b, float scale, uint32_t* out) {
   out[0] = *reinterpret_cast<const uint32_t*>(&lo);
   out[1] = *reinterpret_cast<const uint32_t*>(&hi);
 }
+// What the join needs to know of a sequence.
+struct Share {
+  int32_t splits, tiles;
+  int64_t slot;                     // of its first unit; a sequence of one split has none
+};
 struct CachedArgs {
   const uint8_t *k, *v;
   const float *k_scale, *v_scale;
@@ -22,6 +27,7 @@ struct CachedArgs {
   int64_t ldq, ldo;
   Packed seqs;
   const int32_t *lens, *table;
+  Share* shares;                    // of every sequence, for the join
   float *part, *stats;              // of splits, by slot: O [rows of a tile][HD], and maximum and sum [2][rows]
   int32_t table_ld, pages, kv_heads, group;
   int32_t max_len, resident, least_pages, slots;
@@ -56,13 +62,14 @@ __device__ inline int64_t of_lane(int64_t x, int lane) {
   const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(x), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(x >> 32), lane);
   return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
 }
-__device__ inline int64_t sum_of_wave(int64_t x) {
-  for (int off = 1; off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
+// over the lanes that have a sequence (the others hold 0): `lanes` of them
+__device__ inline int64_t sum_of_wave(int64_t x, int lanes) {
+  for (int off = 1; off < lanes && off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
   return of_lane(x, 0);
 }
 __device__ inline int splits_of(int pages, int split_pages) { return pages > split_pages ? (pages + split_pages - 1) / split_pages : 1; }
-__device__ inline int max_of_wave(int x) {
-  for (int off = 1; off < 64; off <<= 1) x = max(x, __shfl_xor(x, off, 64));
+__device__ inline int max_of_wave(int x, int lanes) {
+  for (int off = 1; off < lanes && off < 64; off <<= 1) x = max(x, __shfl_xor(x, off, 64));
   return __builtin_amdgcn_readlane(x, 0);
 }
 template <int ROWS>
@@ -77,8 +84,8 @@ __device__ inline Deal deal(const CachedArgs& g) {
     work += static_cast<int64_t>(tiles) * pages;
     whole += tiles;
   }
-  work = sum_of_wave(work) * g.kv_heads;
-  whole = sum_of_wave(whole) * g.kv_heads;
+  work = sum_of_wave(work, g.seqs.n) * g.kv_heads;
+  whole = sum_of_wave(whole, g.seqs.n) * g.kv_heads;
   auto pages_for = [&](int64_t ranges) { return static_cast<int>(max(static_cast<int64_t>(g.least_pages), (work + ranges - 1) / ranges)); };
   // units of all sequences, and pages of the longest
   auto count = [&](int split_pages, int64_t* units, int* longest) {
@@ -90,8 +97,8 @@ __device__ inline Deal deal(const CachedArgs& g) {
       sum += static_cast<int64_t>(tiles) * splits;
       if (tiles) most = max(most, (pages + splits - 1) / splits);
     }
-    *units = sum_of_wave(sum) * g.kv_heads;
-    if (longest) *longest = max_of_wave(most);
+    *units = sum_of_wave(sum, g.seqs.n) * g.kv_heads;
+    if (longest) *longest = max_of_wave(most, g.seqs.n);
   };
   const int64_t resident = g.resident;
   if (4 * whole <= resident) {
@@ -116,40 +123,45 @@ __device__ inline Deal deal(const CachedArgs& g) {
   return d;
 }
 // Sequence of unit u, u's number within it and the slot of its first unit.  (u rises through tiles first, then splits, then heads: blocks that
-// run side by side read the same keys.)  With seq >= 0 the slot of that sequence is looked for instead.
+// run side by side read the same keys.)  With `shares` every sequence's are written down instead.
 struct Found {
   int seq, tiles, splits, at;
   int each;                         // pages of a split
   int64_t slot;
 };
 template <int ROWS>
-__device__ inline Found find_unit(const CachedArgs& g, const Deal& d, int64_t u, int seq) {
+__device__ inline Found find_unit(const CachedArgs& g, const Deal& d, int64_t u, Share* shares) {
   const int lane = threadIdx.x & 63;
   Found f{-1, 0, 1, 0, 0, 0};
   int64_t before = 0, slots = 0;
   for (int s0 = 0; s0 < g.seqs.n; s0 += 64) {
-    int tiles = d.tiles, pages = d.pages;
-    if (s0) deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
-    const int splits = splits_of(pages, d.split_pages);
+    int tiles, pages;                 // (looked up again: kept, they would take two registers of every lane through a unit's work)
+    deal_sequence<ROWS>(g, s0 + lane, &tiles, &pages);
+    const int splits = splits_of(pages, d.split_pages), lanes = g.seqs.n - s0;
     const int64_t mine = static_cast<int64_t>(tiles) * splits * g.kv_heads, mine_slots = splits > 1 ? mine : 0;
     int64_t upto = mine, upto_slots = mine_slots;
-    for (int off = 1; off < 64; off <<= 1) {
+    for (int off = 1; off < lanes && off < 64; off <<= 1) {
       const int64_t a = __shfl_up(upto, off, 64), b = __shfl_up(upto_slots, off, 64);
       if (lane >= off) { upto += a; upto_slots += b; }
     }
-    const uint64_t hit = __ballot(seq < 0 ? before + upto > u : s0 + lane == seq);
-    if (hit) {
-      const int l = __builtin_ctzll(hit);
-      f.seq = s0 + l;
-      f.tiles = __builtin_amdgcn_readlane(tiles, l);
-      f.splits = __builtin_amdgcn_readlane(splits, l);
-      f.each = (__builtin_amdgcn_readlane(pages, l) + f.splits - 1) / f.splits;
-      f.at = static_cast<int>(u - before - of_lane(upto - mine, l));
-      f.slot = slots + of_lane(upto_slots - mine_slots, l);
-      return f;
+    if (shares) {
+      if (lane < lanes) shares[s0 + lane] = {splits, tiles, slots + upto_slots - mine_slots};
+    } else {
+      const uint64_t hit = __ballot(lane < lanes && before + upto > u);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        f.seq = s0 + l;
+        f.tiles = __builtin_amdgcn_readlane(tiles, l);
+        f.splits = __builtin_amdgcn_readlane(splits, l);
+        f.each = (__builtin_amdgcn_readlane(pages, l) + f.splits - 1) / f.splits;
+        f.at = static_cast<int>(u - before - of_lane(upto - mine, l));
+        f.slot = slots + of_lane(upto_slots - mine_slots, l);
+        return f;
+      }
     }
-    before += of_lane(upto, 63);
-    slots += of_lane(upto_slots, 63);
+    const int last = lanes < 64 ? lanes - 1 : 63;
+    before += of_lane(upto, last);
+    slots += of_lane(upto_slots, last);
   }
   return f;
 }

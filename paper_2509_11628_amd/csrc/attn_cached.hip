@@ -39,13 +39,14 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
   const Deal d = deal<ROWS>(g);
+  if (g.shares && blockIdx.x == 0 && wave == 0) find_unit<ROWS>(g, d, 0, g.shares);
   // Blocks b, b + 8, ... run on the same XCD: a round of the grid gives each XCD a run of units, which share keys where rows are many.
   const int per_xcd = gridDim.x / 8;
   for (int64_t round = 0;; ++round) {
   const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
   if (round * gridDim.x >= d.units) break;
   if (unit >= d.units) continue;
-  const Found f = find_unit<ROWS>(g, d, unit, -1);
+  const Found f = find_unit<ROWS>(g, d, unit, nullptr);
   if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;        // (offsets that overlap: there is no room for their sums)
   const int tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits, seq = f.seq;
   int start, n;
@@ -367,8 +368,7 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
   packed_rows(g.seqs, seq, &start, &n);
   const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS, rows = static_cast<int64_t>(n) * g.group;
   if (r0 < 0 || r0 + part * quads * 4 >= rows) return;
-  const Deal d = deal<ROWS>(g);
-  const Found f = find_unit<ROWS>(g, d, 0, seq);
+  const Share f = g.shares[seq];
   if (f.splits == 1 || f.slot + static_cast<int64_t>(f.tiles) * f.splits * g.kv_heads > g.slots) return;
   const int64_t first = f.slot + static_cast<int64_t>(head) * f.splits * f.tiles + r0 / ROWS;
   for (int quad = part * quads; quad < (part + 1) * quads && r0 + quad * 4 < rows; ++quad) {
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
     m[half] = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
     off[half] = m[half] == -INFINITY ? 0.0f : m[half] * g.scale_log2e;
   }
-#pragma unroll 4
+#pragma unroll 8
   for (int s = wave; s < f.splits; s += 4)
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -428,7 +428,7 @@ struct Plan {
   int resident, least_pages;
   int64_t tiles, units;             // at most
   int64_t slots;                    // at most; 0: no sequence is long enough to be split
-  int64_t part_bytes, bytes;
+  int64_t part_bytes, stat_bytes, bytes;
 };
 Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int head_dim) {
   Plan p{};
@@ -442,7 +442,8 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   if (pages > p.least_pages) {
     p.slots = std::min<int64_t>(4 * p.resident, whole * ((pages + p.least_pages - 1) / p.least_pages));
     p.part_bytes = p.slots * p.rows * head_dim * static_cast<int64_t>(sizeof(float));
-    p.bytes = p.part_bytes + p.slots * 2 * p.rows * static_cast<int64_t>(sizeof(float));
+    p.stat_bytes = p.slots * 2 * p.rows * static_cast<int64_t>(sizeof(float));
+    p.bytes = p.part_bytes + p.stat_bytes + n_seqs * static_cast<int64_t>(sizeof(Share));
   }
   p.units = whole + p.slots;
   return p;
@@ -513,6 +514,7 @@ Error launch_attention_cached(int dtype, const speca_kv_cache& c, const speca_kv
   g.lens = a.lens; g.table = t.page;
   g.part = static_cast<float*>(workspace);
   g.stats = p.bytes ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes) : nullptr;
+  g.shares = p.bytes ? reinterpret_cast<Share*>(static_cast<char*>(workspace) + p.part_bytes + p.stat_bytes) : nullptr;
   g.table_ld = t.ld; g.pages = c.pages; g.kv_heads = c.kv_heads; g.group = a.heads / c.kv_heads;
   g.max_len = static_cast<int>(std::min<int64_t>(a.max_len, static_cast<int64_t>(t.ld) * PAGE));
   g.resident = p.resident; g.least_pages = p.least_pages; g.slots = static_cast<int32_t>(p.slots);

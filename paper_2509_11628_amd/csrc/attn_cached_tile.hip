@@ -79,7 +79,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
   for (int64_t round = 0; round * gridDim.x < deal_.units; ++round) {
     const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (unit >= deal_.units) continue;
-    const Found f = find_unit<ROWS>(g, deal_, unit, -1);
+    const Found f = find_unit<ROWS>(g, deal_, unit, nullptr);
     if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;      // (offsets that overlap: there is no room for their sums)
     const int row_tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits;
     int start, n;
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     asm volatile("" ::: "memory");                          \
     SPECA_PIN();                                            \
   }
-    constexpr int NS = 4 * KS, NV = 2 * DT, RA = 4, NP = 20;
+    constexpr int NS = 4 * KS, NV = 2 * DT, RA = 2, NP = 20;
     // Tile in buffer `buf`, whose scores lie in sc with their reference known.  NEXT: its successor is page at1 of the sequence, page1 of the cache,
     // whose keys lie in the other buffer and whose values are in va; page2 is the one behind it, whose keys are in ka, and page3 the one behind
     // that.  (Where there is none, some page is loaded and staged, and not used.)
@@ -471,6 +471,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
       }
     }
   }
+  if (g.shares && blockIdx.x == 0 && wave == 0) find_unit<ROWS>(g, deal_, 0, g.shares);
 }
 
 }  // namespace
