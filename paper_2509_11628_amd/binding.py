@@ -297,6 +297,17 @@ def _ints(name, x, like, dims, rows=None, cols=None):
     return x.data_ptr()
 
 
+def _result(x, out):
+    """Where a result of the shape of x goes, and its distance between tokens."""
+    import torch
+    if out is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format), x.shape[1] * x.shape[2]
+    ld = _heads("out", out, x)
+    if out.shape != x.shape:
+        raise ValueError(f"out: {tuple(out.shape)}, q is {tuple(x.shape)}")
+    return out, ld
+
+
 def _stand_alone(like, name, *args):
     """Call an entry point without a context on the current stream of `like`'s device."""
     import torch
@@ -325,39 +336,40 @@ def rope_axes(rope: Rope, positions, q, k=None, q_norm=None, k_norm=None, eps: f
     """speca_rope_axes: q [tokens, heads, head_dim], k [tokens, kv_heads, head_dim] (views of one layer's output, for instance), positions
     int32 [tokens, axes].  -> (q, k) turned, into `out` (a pair, which may be q and k themselves) or new tensors; without k: q alone."""
     import torch
-    sides, made = [], []
-    for i, (name, x, norm) in enumerate((("q", q, q_norm), ("k", k, k_norm))):
-        if x is None:
-            continue
+    tokens, hd = q.shape[0], q.shape[2]
+    if out is not None and not isinstance(out, (tuple, list)):
+        out = (out,)
+    made, sides = [], []
+    for i, x in enumerate((q,) if k is None else (q, k)):
+        name, norm = ("k", k_norm) if i else ("q", q_norm)
         ldx = _heads(name, x, q if i else None)
-        if x.shape[0] != q.shape[0] or x.shape[2] != q.shape[2]:
+        if x.shape[0] != tokens or x.shape[2] != hd:
             raise ValueError(f"{name}: {tuple(x.shape)}, q is {tuple(q.shape)}")
-        if norm is not None and (norm.dtype != q.dtype or norm.device != q.device or tuple(norm.shape) != (q.shape[2],) or not norm.is_contiguous()):
-            raise ValueError(f"{name}_norm: a weight [{q.shape[2]}] of the same type is wanted")
-        o = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out if k is None and not isinstance(out, (tuple, list)) else out[i]
-        ldo = _heads(name + " out", o, q)
-        if o.shape != x.shape:
-            raise ValueError(f"{name} out: {tuple(o.shape)}, {name} is {tuple(x.shape)}")
+        if norm is not None and (norm.dtype is not q.dtype or norm.device != q.device or norm.shape != (hd,) or not norm.is_contiguous()):
+            raise ValueError(f"{name}_norm: a weight [{hd}] of the same type is wanted")
+        if out is None:
+            o = torch.empty_like(x, memory_format=torch.contiguous_format)
+            ldo = x.shape[1] * hd
+        else:
+            o = out[i]
+            ldo = _heads(name + " out", o, q)
+            if o.shape != x.shape:
+                raise ValueError(f"{name} out: {tuple(o.shape)}, {name} is {tuple(x.shape)}")
         made.append(o)
         sides.append(RopeIO(x.data_ptr(), o.data_ptr(), None if norm is None else norm.data_ptr(), ldx, ldo, x.shape[1]))
-    if q.shape[0]:
-        _stand_alone(q, "speca_rope_axes", rope, _ints("positions", positions, q, 2, q.shape[0], rope.axes), q.shape[0], q.shape[2], eps, sides[0],
-                     sides[1] if len(sides) > 1 else None)
-    return tuple(made) if len(made) > 1 else made[0]
+    at = _ints("positions", positions, q, 2, tokens, rope.axes)
+    if tokens:
+        _stand_alone(q, "speca_rope_axes", rope, at, tokens, hd, eps, sides[0], None if k is None else sides[1])
+    return made[0] if k is None else tuple(made)
 
 
 def attention_packed(q, k, v, starts, causal: bool = False, scale: float = 0.0, out=None):
     """speca_attention_packed: q [total, heads, head_dim], k and v [total, kv_heads, head_dim], starts int32 [n_seqs + 1].
     -> [total, heads, head_dim]; tokens outside the sequences are left as they are in `out` (in a new tensor: undefined)."""
-    import torch
     ldq, ldk, ldv = _heads("q", q), _heads("k", k, q), _heads("v", v, q)
     if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]:
         raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)} and v {tuple(v.shape)} do not fit")
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ldo = _heads("out", out, q)
-    if out.shape != q.shape:
-        raise ValueError(f"out: {tuple(out.shape)}, q is {tuple(q.shape)}")
+    out, ldo = _result(q, out)
     at = _ints("starts", starts, q, 1)
     if q.shape[0]:
         _stand_alone(q, "speca_attention_packed", q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, out.data_ptr(), ldo, at, len(starts) - 1,
@@ -414,10 +426,11 @@ def kv_store(cache: KVCache, table, past, k, v, starts):
 def kv_load(cache: KVCache, table, first, starts, total: int, dtype, out=None):
     """speca_kv_load: tokens first[s], first[s] + 1, ... of every sequence -> (k, v) [total, kv_heads, head_dim]; rows outside the
     sequences are left as they are in `out` (a pair; in new tensors: undefined)."""
-    import torch
     if out is None:
-        out = tuple(torch.empty((total, cache.k.shape[1], cache.k.shape[3]), dtype=dtype, device=cache.k.device) for _ in range(2))
-    k, v = out
+        heads, hd = cache.k.shape[1], cache.k.shape[3]
+        k, v = (cache.k.new_empty((total, heads, hd), dtype=dtype) for _ in range(2))
+    else:
+        k, v = out
     ldk, ldv = _heads("k", k), _heads("v", v, k)
     if k.shape != v.shape or k.shape[1] != cache.k.shape[1] or k.shape[0] != total or k.dtype != dtype:
         raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit {total} tokens of {cache.k.shape[1]} key heads in {dtype}")
@@ -430,20 +443,15 @@ def kv_load(cache: KVCache, table, first, starts, total: int, dtype, out=None):
 def attention_cached(q, starts, cache: KVCache, table, lens, causal: bool = True, scale: float = 0.0, max_len: Optional[int] = None, out=None):
     """speca_attention_cached: q bf16 [total, heads, head_dim] over the first lens[s] tokens of their sequence in the cache; max_len: no
     sequence is longer (default: what the table has room for).  -> [total, heads, head_dim]."""
-    import torch
     ldq = _heads("q", q)
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    ldo = _heads("out", out, q)
-    if out.shape != q.shape:
-        raise ValueError(f"out: {tuple(out.shape)}, q is {tuple(q.shape)}")
+    out, ldo = _result(q, out)
     t, at, cu, n = _cached(cache, q, table, lens, starts, "lens")
     total, heads, hd = q.shape
     if not total:
         return out
     longest = table.shape[1] * KV_PAGE if max_len is None else max_len
     size = load_library().speca_attention_cached_workspace(n, total, longest, heads, cache.k.shape[1], hd)
-    room = torch.empty(size, dtype=torch.uint8, device=q.device) if size > 0 else None
+    room = cache.k.new_empty(size) if size > 0 else None
     _stand_alone(q, "speca_attention_cached", q.data_ptr(), ldq, out.data_ptr(), ldo, cu, n, total, cache.desc, t, at, longest, heads, int(causal), scale,
                  None if room is None else room.data_ptr(), max(size, 0))
     return out

@@ -32,9 +32,9 @@ struct RopeArgs {
   int32_t axes, hd, rotated;        // rotated: features that turn
   int32_t heads, total_heads;       // of q, of q and k
   int32_t lanes_per_head;           // power of two, at least hd / (2 VP)
-  int32_t heads_per_wave;           // multiple of 64 / lanes_per_head
+  int32_t steps_per_wave;           // of 64 / lanes_per_head heads
   int32_t chunks;                   // waves per token
-  float eps;
+  float eps, per_feature;           // 1 / hd
   double rate[kMaxHead / 2];        // turns per position of a pair
   uint8_t axis[kMaxHead / 2];
 };
@@ -70,124 +70,137 @@ __device__ inline void rope_write(bf16_t* p, const float (&v)[VP]) {
   else p->bits = static_cast<uint16_t>(cvt_pk_bf16(v[0], v[0]));
 }
 
-// One wave = one token and heads_per_wave of its heads; a lane owns VP pairs of a head and a wave's lanes hold 64 / lanes_per_head heads at a
-// time.  The pieces of a lane are VP features at lo and VP at hi: with HALVES the two sides of its pairs, otherwise neighbours, of which
-// features 2j and 2j + 1 are a pair.
+// VP values at p + lo and VP at p + hi; ahead of the loads, or behind the stores, of a pair of neighbours (ADJACENT) one access of both
+template <int VP, bool HALVES, typename T>
+__device__ inline void rope_load(const T* p, uint32_t lo, uint32_t hi, float (&a)[VP], float (&b)[VP]) {
+  rope_read<VP>(p + lo, a);
+  rope_read<VP>(p + (HALVES || VP == 1 ? hi : lo + VP), b);
+}
+template <int VP, bool HALVES, typename T>
+__device__ inline void rope_store(T* p, uint32_t lo, uint32_t hi, const float (&a)[VP], const float (&b)[VP]) {
+  rope_write<VP>(p + lo, a);
+  rope_write<VP>(p + (HALVES || VP == 1 ? hi : lo + VP), b);
+}
+
+// One wave = one token and some of its heads, steps of 64 / lanes_per_head heads of q, then of k; a lane owns VP pairs of a head.  Its pieces are
+// VP features at lo and VP at hi: with HALVES the two sides of its pairs, otherwise neighbours, of which features 2j and 2j + 1 are a pair.
+// What belongs to the token or the step is in scalar registers, so a lane's addresses are one offset each.
 template <typename T, int VP, bool HALVES, bool NORM>
 __global__ __launch_bounds__(256) void rope_axes_kernel(const RopeArgs g) {
   constexpr int UN = 4;
   const int lane = threadIdx.x & 63;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t item = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t tok = item / g.chunks;
   if (tok >= g.tokens) return;
   const int chunk = static_cast<int>(item - tok * g.chunks);
   const int u = lane & (g.lanes_per_head - 1), sub = lane / g.lanes_per_head, per = 64 / g.lanes_per_head;
   const int units = g.hd / (2 * VP), pairs = g.rotated / 2;
   const bool live = u < units;
-  int lo = u * 2 * VP, hi = lo + VP;
+  uint32_t lo = u * 2 * VP, hi = lo + VP;
   if (HALVES && u * VP < pairs) { lo = u * VP; hi = pairs + lo; }
+  lo += sub * g.hd;
+  hi += sub * g.hd;
 
-  const bool has_q = g.side[0].norm != nullptr, has_k = g.side[1].norm != nullptr;
-  float wq[2 * VP] = {}, wk[2 * VP] = {};
-  if (NORM && live) {
-    float w[VP];
-    const T* const from[2] = {static_cast<const T*>(g.side[0].norm), static_cast<const T*>(g.side[1].norm)};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (!(i ? has_k : has_q)) continue;
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        rope_read<VP>(from[i] + (half ? hi : lo), w);
-#pragma unroll
-        for (int j = 0; j < VP; ++j) (i ? wk : wq)[half * VP + j] = w[j];
-      }
-    }
-  }
+  // The lanes that hold the same pairs of several heads share the work on their angles where there are four of them or more.
   float cs[VP], sn[VP];
-#pragma unroll
-  for (int j = 0; j < VP; ++j) {
-    const int pair = u * VP + j;
-    cs[j] = 1.0f;
-    sn[j] = 0.0f;
+  auto angle = [&](int pair, float* c, float* s) {
+    *c = 1.0f;
+    *s = 0.0f;
     if (pair < pairs) {
       const double turns = static_cast<double>(g.positions[tok * g.axes + g.axis[pair]]) * g.rate[pair];
-      sincospif(2.0f * static_cast<float>(turns - rint(turns)), &sn[j], &cs[j]);
+      sincospif(2.0f * static_cast<float>(turns - rint(turns)), s, c);
     }
+  };
+  if (VP == 4 && per >= 4) {
+    float c, s;
+    angle(u * VP + (sub & 3), &c, &s);
+#pragma unroll
+    for (int j = 0; j < VP; ++j) {
+      cs[j] = __shfl(c, j * g.lanes_per_head + u, 64);
+      sn[j] = __shfl(s, j * g.lanes_per_head + u, 64);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < VP; ++j) angle(u * VP + j, &cs[j], &sn[j]);
   }
-  // UN groups of heads at a time: that many loads are on their way before the first is waited for
-  const int end = min(g.total_heads, (chunk + 1) * g.heads_per_wave);
-  for (int h0 = chunk * g.heads_per_wave + sub; h0 < end; h0 += UN * per) {
-    float a[UN][VP], b[UN][VP];
+
+  int first = chunk * g.steps_per_wave, last = first + g.steps_per_wave;       // steps of this wave, counted from the side's first
 #pragma unroll
-    for (int i = 0; i < UN; ++i) {
-      const int h = h0 + i * per;
-#pragma unroll
-      for (int j = 0; j < VP; ++j) a[i][j] = b[i][j] = 0.0f;
-      if (live && h < end) {
-        const RopeSide& s = g.side[h < g.heads ? 0 : 1];
-        const T* x = static_cast<const T*>(s.x) + tok * s.ldx + static_cast<int64_t>(h < g.heads ? h : h - g.heads) * g.hd;
-        rope_read<VP>(x + lo, a[i]);
-        rope_read<VP>(x + hi, b[i]);
-      }
-    }
-    if (NORM) {
-      float sum[UN];
+  for (int which = 0; which < 2; ++which) {
+    const RopeSide& s = g.side[which];
+    const int heads = which ? g.total_heads - g.heads : g.heads, steps = (heads + per - 1) / per;
+    const int from = first < 0 ? 0 : first, to = last < steps ? last : steps;
+    first -= steps;
+    last -= steps;
+    if (from >= to) continue;
+    const bool norm = NORM && s.norm;
+    float wa[VP] = {}, wb[VP] = {};
+    if (norm && live) rope_load<VP, HALVES>(static_cast<const T*>(s.norm), lo - sub * g.hd, hi - sub * g.hd, wa, wb);
+    const T* x = static_cast<const T*>(s.x) + tok * s.ldx;
+    T* out = static_cast<T*>(s.out) + tok * s.ldo;
+    // UN steps at a time: that many loads are on their way before the first is waited for
+    for (int s0 = from; s0 < to; s0 += UN) {
+      float a[UN][VP], b[UN][VP];
 #pragma unroll
       for (int i = 0; i < UN; ++i) {
-        // pair by pair, then pairs 1, 2, 4, ... apart: the same order, and the same bits, whether a lane holds one pair or four
-        if constexpr (VP == 1) {
-          sum[i] = fmaf(a[i][0], a[i][0], b[i][0] * b[i][0]);
-        } else {
-          const bool across = HALVES && u * VP < pairs;
-          float t[4];
+        const int step = s0 + i;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float x = across ? a[i][j] : j < 2 ? a[i][2 * j] : b[i][2 * j - 4], y = across ? b[i][j] : j < 2 ? a[i][2 * j + 1] : b[i][2 * j - 3];
-            t[j] = fmaf(x, x, y * y);
+        for (int j = 0; j < VP; ++j) a[i][j] = b[i][j] = 0.0f;
+        if (step < to && live && step * per + sub < heads) rope_load<VP, HALVES>(x + step * per * g.hd, lo, hi, a[i], b[i]);
+      }
+      if (norm) {
+        float sum[UN];
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+          // pair by pair, then pairs 1, 2, 4, ... apart: the same order, and the same bits, whether a lane holds one pair or four
+          if constexpr (VP == 1) {
+            sum[i] = fmaf(a[i][0], a[i][0], b[i][0] * b[i][0]);
+          } else {
+            const bool across = HALVES && u * VP < pairs;
+            float t[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float x0 = across ? a[i][j] : j < 2 ? a[i][2 * j] : b[i][2 * j - 4], x1 = across ? b[i][j] : j < 2 ? a[i][2 * j + 1] : b[i][2 * j - 3];
+              t[j] = fmaf(x0, x0, x1 * x1);
+            }
+            sum[i] = (t[0] + t[1]) + (t[2] + t[3]);
           }
-          sum[i] = (t[0] + t[1]) + (t[2] + t[3]);
+        }
+        for (int off = 1; off < g.lanes_per_head; off <<= 1)
+#pragma unroll
+          for (int i = 0; i < UN; ++i) sum[i] += __shfl_xor(sum[i], off, 64);
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+          const float r = rsqrtf(fmaf(sum[i], g.per_feature, g.eps));
+#pragma unroll
+          for (int j = 0; j < VP; ++j) { a[i][j] *= r * wa[j]; b[i][j] *= r * wb[j]; }
         }
       }
-      for (int off = 1; off < g.lanes_per_head; off <<= 1)
-#pragma unroll
-        for (int i = 0; i < UN; ++i) sum[i] += __shfl_xor(sum[i], off, 64);
 #pragma unroll
       for (int i = 0; i < UN; ++i) {
-        const bool of_q = h0 + i * per < g.heads;
-        const float r = rsqrtf(sum[i] / static_cast<float>(g.hd) + g.eps);
-        if (of_q ? has_q : has_k) {
+        const int step = s0 + i;
+        if (step >= to) break;
+        float(&p)[VP] = a[i];
+        float(&q)[VP] = b[i];
+        if constexpr (HALVES || VP == 1) {
 #pragma unroll
-          for (int j = 0; j < VP; ++j) { a[i][j] *= r * (of_q ? wq[j] : wk[j]); b[i][j] *= r * (of_q ? wq[VP + j] : wk[VP + j]); }
+          for (int j = 0; j < VP; ++j) {
+            const float c = fmaf(p[j], cs[j], -(q[j] * sn[j]));
+            q[j] = fmaf(p[j], sn[j], q[j] * cs[j]);
+            p[j] = c;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < VP; j += 2) {
+            const float c = fmaf(p[j], cs[j / 2], -(p[j + 1] * sn[j / 2])), d = fmaf(q[j], cs[VP / 2 + j / 2], -(q[j + 1] * sn[VP / 2 + j / 2]));
+            p[j + 1] = fmaf(p[j], sn[j / 2], p[j + 1] * cs[j / 2]);
+            q[j + 1] = fmaf(q[j], sn[VP / 2 + j / 2], q[j + 1] * cs[VP / 2 + j / 2]);
+            p[j] = c;
+            q[j] = d;
+          }
         }
+        if (live && step * per + sub < heads) rope_store<VP, HALVES>(out + step * per * g.hd, lo, hi, p, q);
       }
-    }
-#pragma unroll
-    for (int i = 0; i < UN; ++i) {
-      const int h = h0 + i * per;
-      if (!live || h >= end) continue;
-      float(&p)[VP] = a[i];
-      float(&q)[VP] = b[i];
-      if constexpr (HALVES || VP == 1) {
-#pragma unroll
-        for (int j = 0; j < VP; ++j) {
-          const float c = fmaf(p[j], cs[j], -(q[j] * sn[j]));
-          q[j] = fmaf(p[j], sn[j], q[j] * cs[j]);
-          p[j] = c;
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < VP; j += 2) {
-          const float c = fmaf(p[j], cs[j / 2], -(p[j + 1] * sn[j / 2])), d = fmaf(q[j], cs[VP / 2 + j / 2], -(q[j + 1] * sn[VP / 2 + j / 2]));
-          p[j + 1] = fmaf(p[j], sn[j / 2], p[j + 1] * cs[j / 2]);
-          q[j + 1] = fmaf(q[j], sn[VP / 2 + j / 2], q[j + 1] * cs[VP / 2 + j / 2]);
-          p[j] = c;
-          q[j] = d;
-        }
-      }
-      const RopeSide& s = g.side[h < g.heads ? 0 : 1];
-      T* out = static_cast<T*>(s.out) + tok * s.ldo + static_cast<int64_t>(h < g.heads ? h : h - g.heads) * g.hd;
-      rope_write<VP>(out + lo, p);
-      rope_write<VP>(out + hi, q);
     }
   }
 }
@@ -256,6 +269,7 @@ Error launch_rope_axes(int dtype, const speca_rope& rope, const int32_t* positio
   g.heads = q.heads;
   g.total_heads = q.heads + (k ? k->heads : 0);
   g.eps = eps;
+  g.per_feature = 1.0f / static_cast<float>(head_dim);
   // rates by repeated multiplication: 128 steps of half a bit of 2^-53 each, far below what a fraction of a turn shows
   int pair = 0;
   for (int a = 0; a < rope.axes; ++a) {
@@ -279,11 +293,11 @@ Error launch_rope_axes(int dtype, const speca_rope& rope, const int32_t* positio
   g.lanes_per_head = 1;
   while (g.lanes_per_head < head_dim / (2 * vp)) g.lanes_per_head *= 2;
   // A wave takes all heads of its token where there are tokens enough for 8 waves per SIMD; with fewer, the heads are dealt to as many waves.
-  const int per = 64 / g.lanes_per_head, steps = (g.total_heads + per - 1) / per;
+  const int per = 64 / g.lanes_per_head, steps = (g.heads + per - 1) / per + (g.total_heads - g.heads + per - 1) / per;
   const int64_t waves = int64_t{32} * compute_units();
   g.chunks = static_cast<int>(std::min<int64_t>(steps, std::max<int64_t>(1, (waves + tokens - 1) / tokens)));
-  g.heads_per_wave = (steps + g.chunks - 1) / g.chunks * per;
-  g.chunks = (g.total_heads + g.heads_per_wave - 1) / g.heads_per_wave;
+  g.steps_per_wave = (steps + g.chunks - 1) / g.chunks;
+  g.chunks = (steps + g.steps_per_wave - 1) / g.steps_per_wave;
   const int64_t blocks = (tokens * g.chunks + 3) / 4;
   if (blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: %lld tokens are too many for one call", static_cast<long long>(tokens));
   if (dtype == SPECA_BF16) launch_t<bf16_t>(g, vp, halves, static_cast<unsigned>(blocks), st);
