@@ -437,7 +437,11 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   p.rows = mean <= 16 ? 16 : mean <= 32 || head_dim < 64 ? 32 : 128;
   p.tiles = rows / p.rows + n_seqs;
   p.resident = 2 * compute_units();
-  p.least_pages = 8;
+  // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (one token of a few
+  // sequences of up to 44 000: 24.9 us, 31.4 with 24), but no splits at all, and no second launch, up to 20 pages (four sequences of up to
+  // 1200: 14 us, 17.5 with splits of 8).  128 rows: 16 (931 + 238 + 16 + 17 tokens over 980, 314, 36 049 and 6026: 77 us, 88 with 8, 85 with 24;
+  // the other way 256 tokens over 4096 and over 1024: 49 us, 39 with 8).
+  p.least_pages = p.rows == 128 ? 16 : pages <= 20 ? 20 : 8;
   const int64_t whole = p.tiles * kv_heads;
   if (pages > p.least_pages) {
     p.slots = std::min<int64_t>(4 * p.resident, whole * ((pages + p.least_pages - 1) / p.least_pages));

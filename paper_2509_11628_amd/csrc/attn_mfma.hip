@@ -154,8 +154,10 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
     head = pair - row * g.H;
     start = static_cast<int64_t>(row) * T;
   } else {
-    head = blockIdx.x % g.H;
-    const int tile = blockIdx.x / g.H, seq = packed_find(g.seqs, tile, 1, 128, 0);
+    const int kv_heads = g.H / g.group, turn = blockIdx.x % g.H;
+    const int each = kv_heads / 8, kv = HD % 64 == 0 || kv_heads % 8 ? turn % kv_heads : turn % 8 * each + turn / 8 % each;
+    head = kv * g.group + turn / kv_heads;
+    const int tile = MODE == CAUSAL ? g.tiles - 1 - static_cast<int>(blockIdx.x) / g.H : static_cast<int>(blockIdx.x) / g.H, seq = packed_find(g.seqs, tile, 1, 128, 0);
     int at;
     packed_rows(g.seqs, seq, &at, &T);
     start = at;
