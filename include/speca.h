@@ -296,8 +296,10 @@ int speca_rope_axes(void* hip_stream, int dtype, const speca_rope* rope, const i
                     float eps, const speca_rope_io* q, const speca_rope_io* k);
 
 /* out = softmax(scale q k^T) v inside every sequence; causal != 0: a token sees itself and the tokens before it.
- * scale 0 = 1 / sqrt(head_dim).  out: [total][heads][head_dim], tokens ldo apart.  head_dim 16, 32, 64, 72 or 128.  What a token
- * does not see has no part in its result, whatever it holds (infinities and NaN included). */
+ * scale 0 = 1 / sqrt(head_dim).  out: [total][heads][head_dim], tokens ldo apart; may not overlap the inputs.  head_dim 16, 32, 64, 72 or 128.  What a
+ * token does not see has no part in its result, whatever it holds (infinities and NaN included).  bf16 runs on the bf16 matrix instructions where
+ * head_dim is 64, 72 or 128, q, k and v are 16-byte aligned with distances of whole 16 bytes (below 2^23 elements for k and v), out 8-byte; on the
+ * fp32 ones, five to ten times slower, elsewhere. */
 int speca_attention_packed(void* hip_stream, int dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                            void* out, int64_t ldo, const int32_t* starts, int n_seqs, int total, int heads, int kv_heads, int head_dim,
                            int causal, float scale);
@@ -332,7 +334,8 @@ typedef struct speca_kv_table {
  * on in its page is cleared.  Two sequences of one call must not write the same page. */
 int speca_kv_store(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* past,
                    const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total);
-/* The other way round: tokens first[s], first[s] + 1, ... of sequence s, as the values they stand for, into packed k and v. */
+/* The other way round: tokens first[s], first[s] + 1, ... of sequence s, as the values they stand for, into packed k and v.  (In both calls a run
+ * that begins below 0 is left out: its tokens are not stored, its rows are left as they are.) */
 int speca_kv_load(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* first,
                   void* k, int64_t ldk, void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total);
 

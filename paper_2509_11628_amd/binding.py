@@ -269,7 +269,7 @@ def _heads(name, x, like=None):
     if like is None:
         if not x.is_cuda or x.dtype not in _storage_types():
             raise ValueError(f"{name}: a bf16 or fp32 device tensor is wanted, got {x.dtype} on {x.device}")
-    elif x.dtype is not like.dtype or x.device != like.device:
+    elif x.dtype is not like.dtype or x.get_device() != like.get_device():
         raise ValueError(f"{name}: {x.dtype} on {x.device}, the others are {like.dtype} on {like.device}")
     return stride[0] if shape[0] > 1 else shape[1] * shape[2]
 
@@ -290,7 +290,7 @@ def _ints(name, x, like, dims, rows=None, cols=None):
     """Address of a contiguous int32 tensor of one or two dimensions on the device of `like`, with as many rows and columns where they are given."""
     import torch
     shape = x.shape
-    if (x.dtype is not torch.int32 or x.device != like.device or len(shape) != dims or not x.is_contiguous()
+    if (x.dtype is not torch.int32 or x.get_device() != like.get_device() or len(shape) != dims or not x.is_contiguous()
             or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols)):
         want = [n if n is not None else "any" for n in (rows, cols)[:dims]]
         raise ValueError(f"{name}: contiguous int32 {want} on {like.device} is wanted, got {x.dtype} {tuple(shape)} on {x.device}")
@@ -384,11 +384,11 @@ class KVCache:
     def __init__(self, k, v, k_scale, v_scale):
         import torch
         p, h, t, hd = k.shape
-        if t != KV_PAGE or tuple(v.shape) != (p, h, hd, t) or tuple(k_scale.shape) != (p, h) or tuple(v_scale.shape) != (p, h):
+        if t != KV_PAGE or v.shape != (p, h, hd, t) or k_scale.shape != (p, h) or v_scale.shape != (p, h):
             raise ValueError(f"pages {tuple(k.shape)} and {tuple(v.shape)} with scales {tuple(k_scale.shape)} and {tuple(v_scale.shape)} do not fit")
-        if k.dtype != torch.uint8 or v.dtype != torch.uint8 or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+        if k.dtype is not torch.uint8 or v.dtype is not torch.uint8 or k_scale.dtype is not torch.float32 or v_scale.dtype is not torch.float32:
             raise ValueError("pages are uint8, their scales fp32")
-        if not (k.is_cuda and k.device == v.device == k_scale.device == v_scale.device and k.is_contiguous() and v.is_contiguous()
+        if not (k.is_cuda and k.get_device() == v.get_device() == k_scale.get_device() == v_scale.get_device() and k.is_contiguous() and v.is_contiguous()
                 and k_scale.is_contiguous() and v_scale.is_contiguous()):
             raise ValueError("pages and scales are contiguous tensors on one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
@@ -405,10 +405,10 @@ class KVCache:
 def _cached(cache, x, table, first, starts, first_name):
     """What the three calls on a cache check alike: the table and the two lists of their sequences."""
     n = len(starts) - 1
-    if x.device != cache.k.device:
+    if x.get_device() != cache.k.get_device():
         raise ValueError(f"tokens on {x.device}, the cache is on {cache.k.device}")
-    if x.shape[2] != cache.k.shape[3]:
-        raise ValueError(f"heads of {x.shape[2]}, the cache's have {cache.k.shape[3]}")
+    if x.shape[2] != cache.desc.head_dim:
+        raise ValueError(f"heads of {x.shape[2]}, the cache's have {cache.desc.head_dim}")
     return KVTable(_ints("table", table, x, 2, n), table.shape[1]), _ints(first_name, first, x, 1, n), _ints("starts", starts, x, 1), n
 
 
@@ -416,8 +416,8 @@ def kv_store(cache: KVCache, table, past, k, v, starts):
     """speca_kv_store: k and v [total, kv_heads, head_dim] become tokens past[s], past[s] + 1, ... of sequence s (rows starts[s] ..
     starts[s + 1]); table int32 [n_seqs, pages of a sequence], past int32 [n_seqs]."""
     ldk, ldv = _heads("k", k), _heads("v", v, k)
-    if k.shape != v.shape or k.shape[1] != cache.k.shape[1]:
-        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit {cache.k.shape[1]} key heads")
+    if k.shape != v.shape or k.shape[1] != cache.desc.kv_heads:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit {cache.desc.kv_heads} key heads")
     t, at, cu, n = _cached(cache, k, table, past, starts, "past")
     if k.shape[0]:
         _stand_alone(k, "speca_kv_store", cache.desc, t, at, k.data_ptr(), ldk, v.data_ptr(), ldv, cu, n, k.shape[0])
@@ -427,13 +427,13 @@ def kv_load(cache: KVCache, table, first, starts, total: int, dtype, out=None):
     """speca_kv_load: tokens first[s], first[s] + 1, ... of every sequence -> (k, v) [total, kv_heads, head_dim]; rows outside the
     sequences are left as they are in `out` (a pair; in new tensors: undefined)."""
     if out is None:
-        heads, hd = cache.k.shape[1], cache.k.shape[3]
+        heads, hd = cache.desc.kv_heads, cache.desc.head_dim
         k, v = (cache.k.new_empty((total, heads, hd), dtype=dtype) for _ in range(2))
     else:
         k, v = out
     ldk, ldv = _heads("k", k), _heads("v", v, k)
-    if k.shape != v.shape or k.shape[1] != cache.k.shape[1] or k.shape[0] != total or k.dtype != dtype:
-        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit {total} tokens of {cache.k.shape[1]} key heads in {dtype}")
+    if k.shape != v.shape or k.shape[1] != cache.desc.kv_heads or k.shape[0] != total or k.dtype != dtype:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} do not fit {total} tokens of {cache.desc.kv_heads} key heads in {dtype}")
     t, at, cu, n = _cached(cache, k, table, first, starts, "first")
     if total:
         _stand_alone(k, "speca_kv_load", cache.desc, t, at, k.data_ptr(), ldk, v.data_ptr(), ldv, cu, n, total)
@@ -450,7 +450,7 @@ def attention_cached(q, starts, cache: KVCache, table, lens, causal: bool = True
     if not total:
         return out
     longest = table.shape[1] * KV_PAGE if max_len is None else max_len
-    size = load_library().speca_attention_cached_workspace(n, total, longest, heads, cache.k.shape[1], hd)
+    size = load_library().speca_attention_cached_workspace(n, total, longest, heads, cache.desc.kv_heads, hd)
     room = cache.k.new_empty(size) if size > 0 else None
     _stand_alone(q, "speca_attention_cached", q.data_ptr(), ldq, out.data_ptr(), ldo, cu, n, total, cache.desc, t, at, longest, heads, int(causal), scale,
                  None if room is None else room.data_ptr(), max(size, 0))

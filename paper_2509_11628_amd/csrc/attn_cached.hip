@@ -1,18 +1,22 @@
-// Attention of new tokens over keys and values in 8-bit pages.
+// Attention of new tokens over keys and values in 8-bit pages: few rows, and the join of split ranges.
 //
 // One block = 16 NQ rows of one (sequence, key head); a row is one query head of one new token, so the heads that share a key head share its
 // reads.  Four waves take the pages w, w + 4, ... of the block's range with an online softmax of their own and merge at the end; where rows are
-// few, the range of keys is split over blocks as well, whose sums a second launch joins.
+// few, the range of keys is split over blocks as well (attn_cached.h), whose sums a second launch joins.
 //   S^T[key][row] = K q^T,  O^T[d][row] += V^T P^T   (bf16 16x16x32 instructions, keys and values widened from e4m3 under their page's
 // scale, exactly: the scale is a power of two)
 // Nothing goes through LDS on its way: a page's layout is the operands' one.  Lane (l, g) of an operand wants 8 of 32 columns of key 16 m + l; it
 // takes 16 bytes at 16 g, which serve two instructions (the order of the columns is a dummy, q follows it).  Of value dimension d it wants the
-// keys in the order in which S^T holds them (4 g .. 4 g + 3 of every 16), which is how the page stores them: 16 bytes per dimension.
+// keys in the order in which S^T holds them (4 g .. 4 g + 3 of every 16), which is how the page stores them: 16 bytes per dimension.  A page's bytes are
+// asked for as soon as the registers of the page before are free: 16 KB per wave and 128 columns, 128 KB per unit, always under way.
+//
+// What bounds it: memory.  One token of 8 sequences of 257 to 65 000 tokens, 32 heads over 8 of 128: 90 us for 437 MB, 4.9 TB/s (a large copy moves 5.0); of one of 65 000
+// 27 us and 8 for the join.  Short ones are a chain of waits: lists, table, bytes, the four waves' sums; four sequences of 1 to 1200 tokens take 10 us.
 #include <algorithm>
 #include <cmath>
 
-#include "gemm.h"
 #include "attn_cached.h"
+#include "gemm.h"
 
 namespace speca {
 
@@ -43,312 +47,312 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
   // Blocks b, b + 8, ... run on the same XCD: a round of the grid gives each XCD a run of units, which share keys where rows are many.
   const int per_xcd = gridDim.x / 8;
   for (int64_t round = 0;; ++round) {
-  const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-  if (round * gridDim.x >= d.units) break;
-  if (unit >= d.units) continue;
-  const Found f = find_unit<ROWS>(g, d, unit, nullptr);
-  if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;        // (offsets that overlap: there is no room for their sums)
-  const int tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits, seq = f.seq;
-  int start, n;
-  packed_rows(g.seqs, seq, &start, &n);
-  const int64_t r0 = static_cast<int64_t>(tile) * ROWS, rows = static_cast<int64_t>(n) * g.group;
-  int len = g.lens[seq];
-  len = len < 0 ? 0 : min(len, g.max_len);
+    const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
+    if (round * gridDim.x >= d.units) break;
+    if (unit >= d.units) continue;
+    const Found f = find_unit<ROWS>(g, d, unit, nullptr);
+    if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;        // (offsets that overlap: there is no room for their sums)
+    const int tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits, seq = f.seq;
+    int start, n;
+    packed_rows(g.seqs, seq, &start, &n);
+    const int64_t r0 = static_cast<int64_t>(tile) * ROWS, rows = static_cast<int64_t>(n) * g.group;
+    int len = g.lens[seq];
+    len = len < 0 ? 0 : min(len, g.max_len);
 
-  // rows 16 i + l16: token, head, number of keys that it sees
-  int tok[NQ], sub[NQ], lim[NQ];
+    // rows 16 i + l16: token, head, number of keys that it sees
+    int tok[NQ], sub[NQ], lim[NQ];
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int64_t r = r0 + i * 16 + l16 < rows ? r0 + i * 16 + l16 : rows - 1;
-    tok[i] = static_cast<int>(r / g.group);
-    sub[i] = static_cast<int>(r - static_cast<int64_t>(tok[i]) * g.group);
-    lim[i] = g.causal ? max(0, len - n + tok[i] + 1) : len;
-  }
-  const int last_tok = static_cast<int>((min(r0 + ROWS, rows) - 1) / g.group), first_tok = static_cast<int>(r0 / g.group);
-  const int most = g.causal ? max(0, len - n + last_tok + 1) : len, least = g.causal ? max(0, len - n + first_tok + 1) : len;
-  const int begin = split * f.each, end = min(begin + f.each, (most + PAGE - 1) / PAGE);
+    for (int i = 0; i < NQ; ++i) {
+      const int64_t r = r0 + i * 16 + l16 < rows ? r0 + i * 16 + l16 : rows - 1;
+      tok[i] = static_cast<int>(r / g.group);
+      sub[i] = static_cast<int>(r - static_cast<int64_t>(tok[i]) * g.group);
+      lim[i] = g.causal ? max(0, len - n + tok[i] + 1) : len;
+    }
+    const int last_tok = static_cast<int>((min(r0 + ROWS, rows) - 1) / g.group), first_tok = static_cast<int>(r0 / g.group);
+    const int most = g.causal ? max(0, len - n + last_tok + 1) : len, least = g.causal ? max(0, len - n + first_tok + 1) : len;
+    const int begin = split * f.each, end = min(begin + f.each, (most + PAGE - 1) / PAGE);
 
-  bf16x8 qf[KS][NQ];
+    bf16x8 qf[KS][NQ];
 #pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const uint16_t* qp = g.q + (static_cast<int64_t>(start) + tok[i]) * g.ldq + (static_cast<int64_t>(head) * g.group + sub[i]) * HD;
+    for (int i = 0; i < NQ; ++i) {
+      const uint16_t* qp = g.q + (static_cast<int64_t>(start) + tok[i]) * g.ldq + (static_cast<int64_t>(head) * g.group + sub[i]) * HD;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int d = s < 2 * FULL ? (s / 2) * 64 + g4 * 16 + (s % 2) * 8 : 64 * FULL + g4 * 8;
-      Frag f;
-      f.u[0] = f.u[1] = f.u[2] = f.u[3] = 0;
-      if (d < HD) {
-        if (g.wide) {
-          const uint4 w = *reinterpret_cast<const uint4*>(qp + d);
-          f.u[0] = w.x; f.u[1] = w.y; f.u[2] = w.z; f.u[3] = w.w;
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) f.u[j] = qp[d + 2 * j] | static_cast<uint32_t>(qp[d + 2 * j + 1]) << 16;
-        }
-      }
-      qf[s][i] = f.v;
-    }
-  }
-
-  floatx4 o[DT][NQ];
-  float mref[NQ], lrun[NQ];
-  bool seen[NQ];
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    mref[i] = -INFINITY;
-    lrun[i] = 0.0f;
-    seen[i] = false;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[dt][i] = floatx4{};
-  }
-
-  const int32_t* table = g.table + static_cast<int64_t>(seq) * g.table_ld;
-  u32x4 kr[4][FULL ? FULL : 1], vr[DT];
-  u32x2 kx[4];
-  float ks = 0.0f, vs = 0.0f;
-  auto load_k = [&](int page) {
-    const int64_t unit = static_cast<int64_t>(page) * g.kv_heads + head;
-    const uint8_t* p = g.k + unit * (PAGE * HD) + l16 * HD;
-    ks = g.k_scale[unit];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-#pragma unroll
-      for (int j = 0; j < FULL; ++j) kr[m][j] = *reinterpret_cast<const u32x4_at8*>(p + m * 16 * HD + j * 64 + g4 * 16);
-      if constexpr (REM > 0) {
-        kx[m] = u32x2{0, 0};
-        if (g4 * 8 < REM) kx[m] = *reinterpret_cast<const u32x2*>(p + m * 16 * HD + FULL * 64 + g4 * 8);
-      }
-    }
-  };
-  auto load_v = [&](int page) {
-    const int64_t unit = static_cast<int64_t>(page) * g.kv_heads + head;
-    const uint8_t* p = g.v + unit * (PAGE * HD) + g4 * 16;
-    vs = g.v_scale[unit];
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const int d = dt * 16 + l16;
-      vr[dt] = *reinterpret_cast<const u32x4*>(p + (d < HD ? d : HD - 1) * PAGE);        // beyond the head: any, never stored
-    }
-  };
-  // Numbers of the wave's next 64 pages, one a lane; those that are not held are passed over.  (Lengths are bounded by the table's row.)
-  int ids = -1, j = begin + wave, ids_from = j;
-  auto fetch_ids = [&] {
-    ids_from = j;
-    const int at = j + 4 * lane;
-    ids = at < end ? table[at] : -1;
-    if (ids >= g.pages) ids = -1;
-  };
-  auto page_at = [&] {                             // of j, or of the first one held behind it
-    for (;;) {
-      if (j >= end) return -1;
-      if (j - ids_from >= 256) fetch_ids();
-      const uint64_t held = __ballot(ids >= 0) >> ((j - ids_from) >> 2);
-      if (held) {
-        j += 4 * __builtin_ctzll(held);
-        return __builtin_amdgcn_readlane(ids, (j - ids_from) >> 2);
-      }
-      j = ids_from + 256;
-    }
-  };
-  fetch_ids();
-  int page = page_at();
-  if (page >= 0) {
-    load_k(page);
-    load_v(page);
-  }
-  while (page >= 0) {
-    const int here = j;
-    j += 4;
-    const int next = page_at();
-    const float vscale = vs;
-    floatx4 s[4][NQ];
-#pragma unroll
-    for (int m = 0; m < 4; ++m) {
-#pragma unroll
-      for (int t = 0; t < KS; ++t) {
+      for (int s = 0; s < KS; ++s) {
+        const int d = s < 2 * FULL ? (s / 2) * 64 + g4 * 16 + (s % 2) * 8 : 64 * FULL + g4 * 8;
         Frag f;
-        if (t < 2 * FULL) {
-          widen(kr[m][t / 2][2 * (t % 2)], ks, f.u);
-          widen(kr[m][t / 2][2 * (t % 2) + 1], ks, f.u + 2);
-        } else {
-          widen(kx[m][0], ks, f.u);
-          widen(kx[m][1], ks, f.u + 2);
-        }
+        f.u[0] = f.u[1] = f.u[2] = f.u[3] = 0;
+        if (d < HD) {
+          if (g.wide) {
+            const uint4 w = *reinterpret_cast<const uint4*>(qp + d);
+            f.u[0] = w.x; f.u[1] = w.y; f.u[2] = w.z; f.u[3] = w.w;
+          } else {
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) s[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[t][i], t ? s[m][i] : floatx4{}, 0, 0, 0);
+            for (int j = 0; j < 4; ++j) f.u[j] = qp[d + 2 * j] | static_cast<uint32_t>(qp[d + 2 * j + 1]) << 16;
+          }
+        }
+        qf[s][i] = f.v;
       }
     }
-    if (next >= 0) load_k(next);                   // its operands are in registers by now
-    const bool edge = (here + 1) * PAGE > least;
-    bool odd = false;                              // the page holds a NaN that some row does not see
-    if (edge) {
+
+    floatx4 o[DT][NQ];
+    float mref[NQ], lrun[NQ];
+    bool seen[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      mref[i] = -INFINITY;
+      lrun[i] = 0.0f;
+      seen[i] = false;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[dt][i] = floatx4{};
+    }
+
+    const int32_t* table = g.table + static_cast<int64_t>(seq) * g.table_ld;
+    u32x4 kr[4][FULL ? FULL : 1], vr[DT];
+    u32x2 kx[4];
+    float ks = 0.0f, vs = 0.0f;
+    auto load_k = [&](int page) {
+      const int64_t unit = static_cast<int64_t>(page) * g.kv_heads + head;
+      const uint8_t* p = g.k + unit * (PAGE * HD) + l16 * HD;
+      ks = g.k_scale[unit];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+#pragma unroll
+        for (int j = 0; j < FULL; ++j) kr[m][j] = *reinterpret_cast<const u32x4_at8*>(p + m * 16 * HD + j * 64 + g4 * 16);
+        if constexpr (REM > 0) {
+          kx[m] = u32x2{0, 0};
+          if (g4 * 8 < REM) kx[m] = *reinterpret_cast<const u32x2*>(p + m * 16 * HD + FULL * 64 + g4 * 8);
+        }
+      }
+    };
+    auto load_v = [&](int page) {
+      const int64_t unit = static_cast<int64_t>(page) * g.kv_heads + head;
+      const uint8_t* p = g.v + unit * (PAGE * HD) + g4 * 16;
+      vs = g.v_scale[unit];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const int d = dt * 16 + l16;
+        vr[dt] = *reinterpret_cast<const u32x4*>(p + (d < HD ? d : HD - 1) * PAGE);        // beyond the head: any, never stored
+      }
+    };
+    // Numbers of the wave's next 64 pages, one a lane; those that are not held are passed over.  (Lengths are bounded by the table's row.)
+    int ids = -1, j = begin + wave, ids_from = j;
+    auto fetch_ids = [&] {
+      ids_from = j;
+      const int at = j + 4 * lane;
+      ids = at < end ? table[at] : -1;
+      if (ids >= g.pages) ids = -1;
+    };
+    auto page_at = [&] {                             // of j, or of the first one held behind it
+      for (;;) {
+        if (j >= end) return -1;
+        if (j - ids_from >= 256) fetch_ids();
+        const uint64_t held = __ballot(ids >= 0) >> ((j - ids_from) >> 2);
+        if (held) {
+          j += 4 * __builtin_ctzll(held);
+          return __builtin_amdgcn_readlane(ids, (j - ids_from) >> 2);
+        }
+        j = ids_from + 256;
+      }
+    };
+    fetch_ids();
+    int page = page_at();
+    if (page >= 0) {
+      load_k(page);
+      load_v(page);
+    }
+    while (page >= 0) {
+      const int here = j;
+      j += 4;
+      const int next = page_at();
+      const float vscale = vs;
+      floatx4 s[4][NQ];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+#pragma unroll
+        for (int t = 0; t < KS; ++t) {
+          Frag f;
+          if (t < 2 * FULL) {
+            widen(kr[m][t / 2][2 * (t % 2)], ks, f.u);
+            widen(kr[m][t / 2][2 * (t % 2) + 1], ks, f.u + 2);
+          } else {
+            widen(kx[m][0], ks, f.u);
+            widen(kx[m][1], ks, f.u + 2);
+          }
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) s[m][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, qf[t][i], t ? s[m][i] : floatx4{}, 0, 0, 0);
+        }
+      }
+      if (next >= 0) load_k(next);                   // its operands are in registers by now
+      const bool edge = (here + 1) * PAGE > least;
+      bool odd = false;                              // the page holds a NaN that some row does not see
+      if (edge) {
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+#pragma unroll
+          for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (here * PAGE + 16 * m + 4 * g4 + e >= lim[i]) s[m][i][e] = -INFINITY;
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {                // bytes past the last token: whatever they are, 0 now
+          const int c = len - (here * PAGE + 16 * m + 4 * g4);
+          const uint32_t keep = c >= 4 ? ~0u : c <= 0 ? 0u : (1u << (8 * c)) - 1u;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            vr[dt][m] &= keep;
+            odd |= (((vr[dt][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
+          }
+        }
+        odd = __any(odd);
+      }
+      bool moved = false;
+      float corr[NQ];
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
+        float top = -INFINITY;
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (here * PAGE + 16 * m + 4 * g4 + e >= lim[i]) s[m][i][e] = -INFINITY;
-      }
+          for (int e = 0; e < 4; ++e) top = fmaxf(top, s[m][i][e]);
+        const float mnew = fmaxf(mref[i], max_of_groups(top));
+        const float moff = mnew == -INFINITY ? 0.0f : mnew * g.scale_log2e;          // no finite score yet: weights 0
+        corr[i] = fast_exp2(mref[i] * g.scale_log2e - moff);
+        moved |= mnew != mref[i];
+        mref[i] = mnew;
+        seen[i] |= here * PAGE < lim[i];
+        float sum = 0.0f;
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {                // bytes past the last token: whatever they are, 0 now
-        const int c = len - (here * PAGE + 16 * m + 4 * g4);
-        const uint32_t keep = c >= 4 ? ~0u : c <= 0 ? 0u : (1u << (8 * c)) - 1u;
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          vr[dt][m] &= keep;
-          odd |= (((vr[dt][m] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0;
-        }
-      }
-      odd = __any(odd);
-    }
-    bool moved = false;
-    float corr[NQ];
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[m][i][e]);
-      const float mnew = fmaxf(mref[i], max_of_groups(top));
-      const float moff = mnew == -INFINITY ? 0.0f : mnew * g.scale_log2e;          // no finite score yet: weights 0
-      corr[i] = fast_exp2(mref[i] * g.scale_log2e - moff);
-      moved |= mnew != mref[i];
-      mref[i] = mnew;
-      seen[i] |= here * PAGE < lim[i];
-      float sum = 0.0f;
-#pragma unroll
-      for (int m = 0; m < 4; ++m)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = fast_exp2(fmaf(s[m][i][e], g.scale_log2e, -moff));
-          s[m][i][e] = p;
-          sum += p;
-        }
-      lrun[i] = lrun[i] * corr[i] + sum;
-    }
-    if (__any(moved)) {
-#pragma unroll
-      for (int i = 0; i < NQ; ++i)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt][i] *= corr[i];
-    }
-    if (odd) {
-      // A NaN counts for the rows that see it and must not meet the probability 0 of the others: it is taken out of the page, and a product of
-      // the places of NaN with the places that a row sees says where it belongs.
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        floatx4 hit[NQ];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          Frag a;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t w = vr[dt][2 * u + h], nan = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-            a.u[2 * h] = (nan & 0x80u ? 0x3F80u : 0u) | (nan & 0x8000u ? 0x3F800000u : 0u);
-            a.u[2 * h + 1] = (nan & 0x800000u ? 0x3F80u : 0u) | (nan & 0x80000000u ? 0x3F800000u : 0u);
-            vr[dt][2 * u + h] = w & ~((nan >> 7) * 0xFFu);
+          for (int e = 0; e < 4; ++e) {
+            const float p = fast_exp2(fmaf(s[m][i][e], g.scale_log2e, -moff));
+            s[m][i][e] = p;
+            sum += p;
           }
-#pragma unroll
-          for (int i = 0; i < NQ; ++i) {
-            Frag b;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int key = here * PAGE + 16 * (2 * u + e / 2) + 4 * g4 + 2 * (e % 2);
-              b.u[e] = (key < lim[i] ? 0x3F80u : 0u) | (key + 1 < lim[i] ? 0x3F800000u : 0u);
-            }
-            hit[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, u ? hit[i] : floatx4{}, 0, 0, 0);
-          }
-        }
+        lrun[i] = lrun[i] * corr[i] + sum;
+      }
+      if (__any(moved)) {
 #pragma unroll
         for (int i = 0; i < NQ; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (hit[i][e] > 0.0f) o[dt][i][e] = __uint_as_float(0x7FC00000u);
+          for (int dt = 0; dt < DT; ++dt) o[dt][i] *= corr[i];
+      }
+      if (odd) {
+        // A NaN counts for the rows that see it and must not meet the probability 0 of the others: it is taken out of the page, and a product of
+        // the places of NaN with the places that a row sees says where it belongs.
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          floatx4 hit[NQ];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            Frag a;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t w = vr[dt][2 * u + h], nan = ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+              a.u[2 * h] = (nan & 0x80u ? 0x3F80u : 0u) | (nan & 0x8000u ? 0x3F800000u : 0u);
+              a.u[2 * h + 1] = (nan & 0x800000u ? 0x3F80u : 0u) | (nan & 0x80000000u ? 0x3F800000u : 0u);
+              vr[dt][2 * u + h] = w & ~((nan >> 7) * 0xFFu);
+            }
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+              Frag b;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int key = here * PAGE + 16 * (2 * u + e / 2) + 4 * g4 + 2 * (e % 2);
+                b.u[e] = (key < lim[i] ? 0x3F80u : 0u) | (key + 1 < lim[i] ? 0x3F800000u : 0u);
+              }
+              hit[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, u ? hit[i] : floatx4{}, 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < NQ; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (hit[i][e] > 0.0f) o[dt][i][e] = __uint_as_float(0x7FC00000u);
+        }
+      }
+      bf16x8 pf[2][NQ];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          Frag f;
+          f.u[0] = cvt_pk_bf16(s[2 * u][i][0], s[2 * u][i][1]);
+          f.u[1] = cvt_pk_bf16(s[2 * u][i][2], s[2 * u][i][3]);
+          f.u[2] = cvt_pk_bf16(s[2 * u + 1][i][0], s[2 * u + 1][i][1]);
+          f.u[3] = cvt_pk_bf16(s[2 * u + 1][i][2], s[2 * u + 1][i][3]);
+          pf[u][i] = f.v;
+        }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Frag f;
+          widen(vr[dt][2 * u], vscale, f.u);
+          widen(vr[dt][2 * u + 1], vscale, f.u + 2);
+#pragma unroll
+          for (int i = 0; i < NQ; ++i) o[dt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, pf[u][i], o[dt][i], 0, 0, 0);
+        }
+      if (next >= 0) load_v(next);
+      page = next;
+    }
+
+    // together: everything relative to the largest maximum of the four waves; wave w sums the dimensions of tiles w, w + 4, ...
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      const float l = sum_of_groups(lrun[i]);
+      if (g4 == 0) {
+        stat_m[wave][i * 16 + l16] = mref[i];
+        stat_l[wave][i * 16 + l16] = l;
+        stat_seen[wave][i * 16 + l16] = seen[i] ? 1.0f : 0.0f;
       }
     }
-    bf16x8 pf[2][NQ];
+    __syncthreads();
+    float top[NQ], total[NQ];
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < NQ; ++i) {
+      const int r = i * 16 + l16;
+      top[i] = fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
+      const float off = top[i] == -INFINITY ? 0.0f : top[i] * g.scale_log2e;
+      total[i] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) total[i] += stat_l[w][r] * fast_exp2(stat_m[w][r] * g.scale_log2e - off);
+      // keys were there, none with a score above -inf: that has no softmax.  No keys: 0
+      if (top[i] == -INFINITY) total[i] = stat_seen[0][r] + stat_seen[1][r] + stat_seen[2][r] + stat_seen[3][r] > 0.0f ? __uint_as_float(0x7FC00000u) : 0.0f;
+      const float f = fast_exp2(mref[i] * g.scale_log2e - off);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) merge[wave][dt * NQ + i][lane] = o[dt][i] * f;
+    }
+    __syncthreads();
+    const int64_t slot = f.slot + f.at;
+    if (f.splits > 1 && wave == 0 && g4 == 0) {
 #pragma unroll
       for (int i = 0; i < NQ; ++i) {
-        Frag f;
-        f.u[0] = cvt_pk_bf16(s[2 * u][i][0], s[2 * u][i][1]);
-        f.u[1] = cvt_pk_bf16(s[2 * u][i][2], s[2 * u][i][3]);
-        f.u[2] = cvt_pk_bf16(s[2 * u + 1][i][0], s[2 * u + 1][i][1]);
-        f.u[3] = cvt_pk_bf16(s[2 * u + 1][i][2], s[2 * u + 1][i][3]);
-        pf[u][i] = f.v;
-      }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        Frag f;
-        widen(vr[dt][2 * u], vscale, f.u);
-        widen(vr[dt][2 * u + 1], vscale, f.u + 2);
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) o[dt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.v, pf[u][i], o[dt][i], 0, 0, 0);
-      }
-    if (next >= 0) load_v(next);
-    page = next;
-  }
-
-  // together: everything relative to the largest maximum of the four waves; wave w sums the dimensions of tiles w, w + 4, ...
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const float l = sum_of_groups(lrun[i]);
-    if (g4 == 0) {
-      stat_m[wave][i * 16 + l16] = mref[i];
-      stat_l[wave][i * 16 + l16] = l;
-      stat_seen[wave][i * 16 + l16] = seen[i] ? 1.0f : 0.0f;
-    }
-  }
-  __syncthreads();
-  float top[NQ], total[NQ];
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) {
-    const int r = i * 16 + l16;
-    top[i] = fmaxf(fmaxf(stat_m[0][r], stat_m[1][r]), fmaxf(stat_m[2][r], stat_m[3][r]));
-    const float off = top[i] == -INFINITY ? 0.0f : top[i] * g.scale_log2e;
-    total[i] = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) total[i] += stat_l[w][r] * fast_exp2(stat_m[w][r] * g.scale_log2e - off);
-    // keys were there, none with a score above -inf: that has no softmax.  No keys: 0
-    if (top[i] == -INFINITY) total[i] = stat_seen[0][r] + stat_seen[1][r] + stat_seen[2][r] + stat_seen[3][r] > 0.0f ? __uint_as_float(0x7FC00000u) : 0.0f;
-    const float f = fast_exp2(mref[i] * g.scale_log2e - off);
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) merge[wave][dt * NQ + i][lane] = o[dt][i] * f;
-  }
-  __syncthreads();
-  const int64_t slot = f.slot + f.at;
-  if (f.splits > 1 && wave == 0 && g4 == 0) {
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      g.stats[slot * 2 * ROWS + i * 16 + l16] = top[i];
-      g.stats[slot * 2 * ROWS + ROWS + i * 16 + l16] = total[i];
-    }
-  }
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    if (dt % 4 != wave) continue;
-    const int d = dt * 16 + 4 * g4;
-    if (d >= HD) continue;
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      const floatx4 v = (merge[0][dt * NQ + i][lane] + merge[1][dt * NQ + i][lane]) + (merge[2][dt * NQ + i][lane] + merge[3][dt * NQ + i][lane]);
-      if (f.splits > 1) {
-        *reinterpret_cast<floatx4*>(g.part + (slot * ROWS + i * 16 + l16) * HD + d) = v;
-      } else if (r0 + i * 16 + l16 < rows) {
-        uint16_t* op = g.out + (static_cast<int64_t>(start) + tok[i]) * g.ldo + (static_cast<int64_t>(head) * g.group + sub[i]) * HD + d;
-        const float inv = total[i] == 0.0f ? 0.0f : 1.0f / total[i];
-        const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
-        if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
-        else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+        g.stats[slot * 2 * ROWS + i * 16 + l16] = top[i];
+        g.stats[slot * 2 * ROWS + ROWS + i * 16 + l16] = total[i];
       }
     }
-  }
-  __syncthreads();                                 // the next unit writes the statistics again
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      if (dt % 4 != wave) continue;
+      const int d = dt * 16 + 4 * g4;
+      if (d >= HD) continue;
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) {
+        const floatx4 v = (merge[0][dt * NQ + i][lane] + merge[1][dt * NQ + i][lane]) + (merge[2][dt * NQ + i][lane] + merge[3][dt * NQ + i][lane]);
+        if (f.splits > 1) {
+          *reinterpret_cast<floatx4*>(g.part + (slot * ROWS + i * 16 + l16) * HD + d) = v;
+        } else if (r0 + i * 16 + l16 < rows) {
+          uint16_t* op = g.out + (static_cast<int64_t>(start) + tok[i]) * g.ldo + (static_cast<int64_t>(head) * g.group + sub[i]) * HD + d;
+          const float inv = total[i] == 0.0f ? 0.0f : 1.0f / total[i];
+          const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
+          if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
+          else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+        }
+      }
+    }
+    __syncthreads();                                 // the next unit writes the statistics again
   }
 }
 
@@ -372,54 +376,54 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
   if (f.splits == 1 || f.slot + static_cast<int64_t>(f.tiles) * f.splits * g.kv_heads > g.slots) return;
   const int64_t first = f.slot + static_cast<int64_t>(head) * f.splits * f.tiles + r0 / ROWS;
   for (int quad = part * quads; quad < (part + 1) * quads && r0 + quad * 4 < rows; ++quad) {
-  auto stat = [&](int s, int which, int r) { return g.stats[((first + static_cast<int64_t>(s) * f.tiles) * 2 + which) * ROWS + quad * 4 + r]; };
+    auto stat = [&](int s, int which, int r) { return g.stats[((first + static_cast<int64_t>(s) * f.tiles) * 2 + which) * ROWS + quad * 4 + r]; };
 
-  float top = -INFINITY;                           // of row lane % 4, over the splits of this lane, then of all
-  for (int s = tid >> 2; s < f.splits; s += 64) top = fmaxf(top, stat(s, 0, tid & 3));
-  for (int off = 4; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-  if (lane < 4) tops[wave][lane] = top;
-  __syncthreads();
-  const int col = lane & 31;
-  float m[2], off[2], total[2] = {};
-  floatx4 v[2] = {};
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int r = 2 * half + (lane >> 5);
-    m[half] = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
-    off[half] = m[half] == -INFINITY ? 0.0f : m[half] * g.scale_log2e;
-  }
-#pragma unroll 8
-  for (int s = wave; s < f.splits; s += 4)
+    float top = -INFINITY;                           // of row lane % 4, over the splits of this lane, then of all
+    for (int s = tid >> 2; s < f.splits; s += 64) top = fmaxf(top, stat(s, 0, tid & 3));
+    for (int off = 4; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    if (lane < 4) tops[wave][lane] = top;
+    __syncthreads();
+    const int col = lane & 31;
+    float m[2], off[2], total[2] = {};
+    floatx4 v[2] = {};
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int r = 2 * half + (lane >> 5);
-      const float ms = stat(s, 0, r), l = stat(s, 1, r);
-      const floatx4 x = *reinterpret_cast<const floatx4*>(g.part + ((first + static_cast<int64_t>(s) * f.tiles) * ROWS + quad * 4 + r) * HD + 4 * (col < C ? col : 0));
-      // a split without a finite score has weight 0, unless all are so: then NaN where keys were seen, 0 elsewhere
-      const float w = ms == -INFINITY ? (m[half] == -INFINITY ? 1.0f : 0.0f) : fast_exp2(ms * g.scale_log2e - off[half]);
-      total[half] += ms == -INFINITY && w == 0.0f ? 0.0f : l * w;
-      v[half] += x * w;
+      m[half] = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+      off[half] = m[half] == -INFINITY ? 0.0f : m[half] * g.scale_log2e;
     }
+#pragma unroll 8
+    for (int s = wave; s < f.splits; s += 4)
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int r = 2 * half + (lane >> 5);
-    if (col < C) sums[wave][r][col] = v[half];
-    if (col == 0) totals[wave][r] = total[half];
-  }
-  __syncthreads();
-  const int r = tid / C, c = tid - r * C;
-  if (tid < 4 * C && r0 + quad * 4 + r < rows) {
-  const floatx4 v = (sums[0][r][c] + sums[1][r][c]) + (sums[2][r][c] + sums[3][r][c]);
-  const float total = (totals[0][r] + totals[1][r]) + (totals[2][r] + totals[3][r]);
-  const int64_t row = r0 + quad * 4 + r;
-  const int tok = static_cast<int>(row / g.group), sub = static_cast<int>(row - static_cast<int64_t>(tok) * g.group);
-  uint16_t* op = g.out + (static_cast<int64_t>(start) + tok) * g.ldo + (static_cast<int64_t>(head) * g.group + sub) * HD + 4 * c;
-  const float inv = total == 0.0f ? 0.0f : 1.0f / total;
-  const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
-  if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
-  else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
-  }
-  __syncthreads();
+      for (int half = 0; half < 2; ++half) {
+        const int r = 2 * half + (lane >> 5);
+        const float ms = stat(s, 0, r), l = stat(s, 1, r);
+        const floatx4 x = *reinterpret_cast<const floatx4*>(g.part + ((first + static_cast<int64_t>(s) * f.tiles) * ROWS + quad * 4 + r) * HD + 4 * (col < C ? col : 0));
+        // a split without a finite score has weight 0, unless all are so: then NaN where keys were seen, 0 elsewhere
+        const float w = ms == -INFINITY ? (m[half] == -INFINITY ? 1.0f : 0.0f) : fast_exp2(ms * g.scale_log2e - off[half]);
+        total[half] += ms == -INFINITY && w == 0.0f ? 0.0f : l * w;
+        v[half] += x * w;
+      }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const int r = 2 * half + (lane >> 5);
+      if (col < C) sums[wave][r][col] = v[half];
+      if (col == 0) totals[wave][r] = total[half];
+    }
+    __syncthreads();
+    const int r = tid / C, c = tid - r * C;
+    if (tid < 4 * C && r0 + quad * 4 + r < rows) {
+      const floatx4 v = (sums[0][r][c] + sums[1][r][c]) + (sums[2][r][c] + sums[3][r][c]);
+      const float total = (totals[0][r] + totals[1][r]) + (totals[2][r] + totals[3][r]);
+      const int64_t row = r0 + quad * 4 + r;
+      const int tok = static_cast<int>(row / g.group), sub = static_cast<int>(row - static_cast<int64_t>(tok) * g.group);
+      uint16_t* op = g.out + (static_cast<int64_t>(start) + tok) * g.ldo + (static_cast<int64_t>(head) * g.group + sub) * HD + 4 * c;
+      const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+      const uint32_t a = cvt_pk_bf16(v[0] * inv, v[1] * inv), b = cvt_pk_bf16(v[2] * inv, v[3] * inv);
+      if (g.wide) *reinterpret_cast<uint2*>(op) = make_uint2(a, b);
+      else { op[0] = static_cast<uint16_t>(a); op[1] = static_cast<uint16_t>(a >> 16); op[2] = static_cast<uint16_t>(b); op[3] = static_cast<uint16_t>(b >> 16); }
+    }
+    __syncthreads();
   }
 }
 
