@@ -116,7 +116,7 @@ __device__ __forceinline__ void buffer_to_lds(const uint16_t* buffer, int bytes,
 
 // Rows of equal length (PLAIN), or packed sequences, of which causal tokens see themselves and those before them.
 // Packed, one MI355X: 5 sequences of 589 to 4608 tokens, 24 heads of 128: 605 to 640 us, 950 to 1010 TFLOP/s (power, as above); 12 causal ones of 19 to 4096, 32 heads over
-// 8 of 128: 350 to 365 us, 775 to 810 TFLOP/s of the products that count (a block's last two tiles are half hidden); 16 of 1 to 400 tokens, 16 heads of
+// 8 of 128: 334 to 345 us, 820 to 845 TFLOP/s of the products that count (a block's last two tiles are half hidden); 16 of 1 to 400 tokens, 16 heads of
 // 72: 17.5 us, a chain of waits (places, first tiles, up to 7 tiles), in which the keys of several heads a cache line go to one XCD.
 enum { PLAIN = 0, PACKED = 1, CAUSAL = 2 };
 struct TileArgs {
@@ -303,30 +303,26 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
     for (int i = 0; i < 32; ++i)
       if (kt * 64 + (i >> 3) * 16 + 4 * g4 + (i & 3) > last_key((i >> 2) & 1)) s[i >> 3][(i >> 2) & 1][i & 3] = -INFINITY;
   };
-  // A value that is no number must not meet the probability 0 of a causal query that does not see it.  Where the tile that a wave's queries see
-  // in part holds one, it is taken out of the product, and products of the places of +inf, -inf and NaN (among the words w of a fragment)
-  // with the places that a query sees say where it belongs.
-  auto odd_values = [&](const uint32_t* w, int words, auto&& product, floatx4& to) {
-    floatx4 hit[3];
+  // A value that is no number must not meet the probability 0 of a causal query that does not see it: in the tile that a wave's queries see in
+  // part, where there is one, it counts as 0 in the product, and for the queries that see it is added here.
+  auto add_odd = [&](int from, int to) {                           // of keys from .. to - 1
 #pragma unroll
-    for (int kind = 0; kind < 3; ++kind) {
-      uint32_t at[4] = {};
+    for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int i = 0; i < words; ++i)
+      for (int e = 0; e < 4; ++e) {
+        const int d = dt * 16 + 4 * g4 + e < HD ? dt * 16 + 4 * g4 + e : HD - 1;
+        float add[2] = {};
+#pragma unroll 1
+        for (int key = from; key < to && key < T; ++key) {
+          const uint16_t x = vb[key * g.ldv + d];
+          if ((x & 0x7F80) != 0x7F80) continue;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t x = (w[i] >> (16 * h)) & 0xFFFFu;
-          const bool yes = kind == 0 ? x == 0x7F80u : kind == 1 ? x == 0xFF80u : (x & 0x7FFFu) > 0x7F80u;
-          at[i] |= yes ? 0x3F80u << (16 * h) : 0u;
+          for (int n = 0; n < 2; ++n)
+            if (key <= last_key(n)) add[n] += bf16_to_f32(x);
         }
-      hit[kind] = product(at);
-    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (hit[0][e] > 0.0f) to[e] += INFINITY;
-      if (hit[1][e] > 0.0f) to[e] -= INFINITY;
-      if (hit[2][e] > 0.0f) to[e] = __uint_as_float(0x7FC00000u);
-    }
+        for (int n = 0; n < 2; ++n) o[dt][n][e] += add[n];
+      }
   };
 
   // Ring: keys are fetched two tiles ahead, values one.  At the top of tile kt the wave's outstanding loads are K(kt + 1) and V(kt);
@@ -347,6 +343,7 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
     // other in a single wave, the block would take half as long as a whole one).  Second contraction by 16x16x16 instructions.
     floatx4 s[2];
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {};
+    uint32_t odd = 0;
     issue_k(0);
     issue_v(0);
     for (int kt = 0; kt < ntiles; ++kt) {
@@ -390,30 +387,16 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
       for (int dt = 0; dt < DT; ++dt) {
         union { uint32_t u[2]; short4v v; } vf;
         vf.v = value_half(kt & 1, 16 * wave, dt);
-        if (MODE == CAUSAL && kt + 1 == ntiles && __any((odd_halves(vf.u[0]) | odd_halves(vf.u[1])) != 0)) {
-          const uint32_t w[2] = {vf.u[0], vf.u[1]};
-          vf.u[0] = without_odd(w[0]);
-          vf.u[1] = without_odd(w[1]);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            o[dt][n] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf.v, pf[n], o[dt][n], 0, 0, 0);
-            odd_values(w, 2, [&](const uint32_t* at) {
-              union { uint32_t u[2]; short4v v; } a, b;
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const int key = kt * 64 + 16 * wave + 4 * g4 + 2 * i;
-                a.u[i] = at[i];
-                b.u[i] = (key <= last_key(n) ? 0x3F80u : 0u) | (key + 1 <= last_key(n) ? 0x3F800000u : 0u);
-              }
-              return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(a.v, b.v, floatx4{}, 0, 0, 0);
-            }, o[dt][n]);
-          }
-          continue;
+        if (MODE == CAUSAL && kt + 1 == ntiles) {
+          odd |= odd_halves(vf.u[0]) | odd_halves(vf.u[1]);
+          vf.u[0] = without_odd(vf.u[0]);
+          vf.u[1] = without_odd(vf.u[1]);
         }
 #pragma unroll
         for (int n = 0; n < 2; ++n) o[dt][n] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf.v, pf[n], o[dt][n], 0, 0, 0);
       }
     }
+    if (MODE == CAUSAL && __any(odd != 0)) add_odd((ntiles - 1) * 64 + 16 * wave, (ntiles - 1) * 64 + 16 * wave + 16);
     // together: everything relative to the largest maximum, then waves 1 .. 3 hand their sums to wave 0 through LDS
     float* stat = reinterpret_cast<float*>(smem);
     SPECA_TURN()
@@ -483,44 +466,17 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
       }
     }
     psum[0] = psum[1] = 0.0f;
+    bool odd = false;                       // some value of the tile that the wave sees in part is no number
+    union Words { bf16x8 v; uint32_t u[4]; };
     if constexpr (!NEXT && MODE == CAUSAL) {
-      union Words { bf16x8 v; uint32_t u[4]; };
       uint32_t any = 0;
-      int from = buf;                       // read again further down, rather than kept from here
-      asm volatile("" : "+s"(from));
 #pragma unroll
       for (int i = 0; i < NV; ++i) {
         Words x;
         x.v = value_frag(buf, i / DT, i % DT);
         any |= odd_halves(x.u[0]) | odd_halves(x.u[1]) | odd_halves(x.u[2]) | odd_halves(x.u[3]);
       }
-      if (__any(any != 0)) {
-        probabilities(sc, 0, 32);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          Words x, y;
-          x.v = value_frag(from, i / DT, i % DT);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) y.u[j] = without_odd(x.u[j]);
-#pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            o[i % DT][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y.v, pack(sc, i / DT, n), o[i % DT][n], 0, 0, 0);
-            odd_values(x.u, 4, [&](const uint32_t* at) {
-              Words a, b;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const int key = kt * 64 + 32 * (i / DT) + 16 * (j >> 1) + 4 * g4 + 2 * (j & 1);
-                a.u[j] = at[j];
-                b.u[j] = (key <= last_key(n) ? 0x3F80u : 0u) | (key + 1 <= last_key(n) ? 0x3F800000u : 0u);
-              }
-              return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, floatx4{}, 0, 0, 0);
-            }, o[i % DT][n]);
-          }
-        }
-#pragma unroll
-        for (int n = 0; n < 2; ++n) lrun[n] += psum[n];
-        return;
-      }
+      odd = __any(any != 0);
     }
     if constexpr (NEXT) {
 #pragma unroll
@@ -555,6 +511,15 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
       for (int n = 0; n < 2; ++n) {
         if (i < DT) probabilities(sc, NP + (2 * i + n) * (32 - NP) / (2 * DT - 1), i + 1 == DT && n ? 32 : NP + (2 * i + n + 1) * (32 - NP) / (2 * DT - 1));
         else if constexpr (NEXT) maximum(sn, (2 * (i - DT) + n) * 32 / (2 * DT), (2 * (i - DT) + n + 1) * 32 / (2 * DT));
+        if constexpr (!NEXT && MODE == CAUSAL) {
+          if (n == 0 && odd) {
+            Words x;
+            x.v = vf[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.u[j] = without_odd(x.u[j]);
+            vf[i] = x.v;
+          }
+        }
         SPECA_PIN();
         o[i % DT][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pf[i / DT][n], o[i % DT][n], 0, 0, 0);
         SPECA_PIN();
@@ -562,6 +527,7 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
     }
 #pragma unroll
     for (int n = 0; n < 2; ++n) lrun[n] += psum[n];
+    if (MODE == CAUSAL && odd) add_odd(kt * 64, kt * 64 + 64);
     if constexpr (NEXT) reference();
   };
   // tile kt, not the last one, in buffer PAR = kt % 2, its scores in SC
