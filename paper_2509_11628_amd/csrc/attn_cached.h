@@ -35,9 +35,10 @@ struct CachedArgs {
   float scale_log2e;
 };
 
-// How the work is dealt.  The host knows no lengths, so every wave works it out from the lists on the device, 64 sequences at a time.  A unit is
-// one row tile of one key head over one split of its sequence's range of pages; ranges longer than split_pages are split evenly.  With `whole` units
-// if nothing is split and W pages to visit in all, split_pages = W / E makes at most min(E + whole, 2 E) units of split ranges.
+// How the work is dealt.  The host knows no lengths, so every wave works it out from the lists on the device, 64 sequences at a time.  A
+// unit is one row tile of one key head over one split of its sequence's range of pages; ranges longer than split_pages are split evenly.
+// With `whole` units if nothing is split and W pages to visit in all, split_pages = W / E makes at most min(E + whole, 2 E) units of split
+// ranges.
 //   whole <= resident / 4:  E = resident - whole: one round of the blocks that fit on the chip
 //   otherwise:              E = R resident - whole for the R of 1 to 4 whose rounds x (longest unit + 4 pages that it takes to begin and end one) are
 //                           fewest (E = 2 resident where no R has room)
@@ -122,8 +123,8 @@ __device__ inline Deal deal(const CachedArgs& g) {
   }
   return d;
 }
-// Sequence of unit u, u's number within it and the slot of its first unit.  (u rises through tiles first, then splits, then heads: blocks that
-// run side by side read the same keys.)  With `shares` every sequence's are written down instead.
+// Sequence of unit u, u's number within it and the slot of its first unit.  (u rises through tiles first, then splits, then heads: blocks
+// that run side by side read the same keys.)  With `shares` every sequence's are written down instead.
 struct Found {
   int seq, tiles, splits, at;
   int each;                         // pages of a split
@@ -165,6 +166,9 @@ __device__ inline Found find_unit(const CachedArgs& g, const Deal& d, int64_t u,
   }
   return f;
 }
+
+// Keys that new token `tok` of n sees, of `held` in the sequence of which the first `len` count.
+__device__ inline int keys_of(const CachedArgs& g, int held, int len, int n, int tok) { return g.causal ? max(0, min(len, held - n + tok + 1)) : len; }
 
 // 128 rows a tile, head_dim 64, 72 or 128 (attn_cached_tile.hip).
 void launch_attention_cached_tile(const CachedArgs& g, int head_dim, unsigned blocks, hipStream_t st);

@@ -1,17 +1,19 @@
 // Attention of new tokens over keys and values in 8-bit pages: few rows, and the join of split ranges.
 //
 // One block = 16 NQ rows of one (sequence, key head); a row is one query head of one new token, so the heads that share a key head share its
-// reads.  Four waves take the pages w, w + 4, ... of the block's range with an online softmax of their own and merge at the end; where rows are
-// few, the range of keys is split over blocks as well (attn_cached.h), whose sums a second launch joins.
+// reads.  Four waves take the pages w, w + 4, ... of the block's range with an online softmax of their own and merge at the end; where rows
+// are few, the range of keys is split over blocks as well (attn_cached.h), whose sums a second launch joins.
 //   S^T[key][row] = K q^T,  O^T[d][row] += V^T P^T   (bf16 16x16x32 instructions, keys and values widened from e4m3 under their page's
 // scale, exactly: the scale is a power of two)
-// Nothing goes through LDS on its way: a page's layout is the operands' one.  Lane (l, g) of an operand wants 8 of 32 columns of key 16 m + l; it
-// takes 16 bytes at 16 g, which serve two instructions (the order of the columns is a dummy, q follows it).  Of value dimension d it wants the
-// keys in the order in which S^T holds them (4 g .. 4 g + 3 of every 16), which is how the page stores them: 16 bytes per dimension.  A page's bytes are
-// asked for as soon as the registers of the page before are free: 16 KB per wave and 128 columns, 128 KB per unit, always under way.
+// Nothing goes through LDS on its way: a page's layout is the operands' one.  Lane (l, g) of an operand wants 8 of 32 columns of key 16 m +
+// l; it takes 16 bytes at 16 g, which serve two instructions (the order of the columns is a dummy, q follows it).  Of value dimension d it
+// wants the keys in the order in which S^T holds them (4 g .. 4 g + 3 of every 16), which is how the page stores them: 16 bytes per
+// dimension.  A page's bytes are asked for as soon as the registers of the page before are free: 16 KB per wave and 128 columns, 128 KB per
+// unit, always under way.
 //
-// What bounds it: memory.  One token of 8 sequences of 257 to 65 000 tokens, 32 heads over 8 of 128: 90 us for 437 MB, 4.9 TB/s (a large copy moves 5.0); of one of 65 000
-// 27 us and 8 for the join.  Short ones are a chain of waits: lists, table, bytes, the four waves' sums; four sequences of 1 to 1200 tokens take 10 us.
+// What bounds it: memory.  One token of 8 sequences of 257 to 65 000 tokens, 32 heads over 8 of 128: 90 us for 437 MB, 4.9 TB/s (a large
+// copy moves 5.0); of one of 65 000 27 us and 8 for the join.  Short ones are a chain of waits: lists, table, bytes, the four waves' sums;
+// four sequences of 1 to 1200 tokens take 10 us.
 #include <algorithm>
 #include <cmath>
 
@@ -56,8 +58,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
     int start, n;
     packed_rows(g.seqs, seq, &start, &n);
     const int64_t r0 = static_cast<int64_t>(tile) * ROWS, rows = static_cast<int64_t>(n) * g.group;
-    int len = g.lens[seq];
-    len = len < 0 ? 0 : min(len, g.max_len);
+    const int held = max(0, g.lens[seq]), len = min(held, g.max_len);
 
     // rows 16 i + l16: token, head, number of keys that it sees
     int tok[NQ], sub[NQ], lim[NQ];
@@ -66,10 +67,10 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
       const int64_t r = r0 + i * 16 + l16 < rows ? r0 + i * 16 + l16 : rows - 1;
       tok[i] = static_cast<int>(r / g.group);
       sub[i] = static_cast<int>(r - static_cast<int64_t>(tok[i]) * g.group);
-      lim[i] = g.causal ? max(0, len - n + tok[i] + 1) : len;
+      lim[i] = keys_of(g, held, len, n, tok[i]);
     }
     const int last_tok = static_cast<int>((min(r0 + ROWS, rows) - 1) / g.group), first_tok = static_cast<int>(r0 / g.group);
-    const int most = g.causal ? max(0, len - n + last_tok + 1) : len, least = g.causal ? max(0, len - n + first_tok + 1) : len;
+    const int most = keys_of(g, held, len, n, last_tok), least = keys_of(g, held, len, n, first_tok);
     const int begin = split * f.each, end = min(begin + f.each, (most + PAGE - 1) / PAGE);
 
     bf16x8 qf[KS][NQ];
@@ -239,8 +240,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
           for (int dt = 0; dt < DT; ++dt) o[dt][i] *= corr[i];
       }
       if (odd) {
-        // A NaN counts for the rows that see it and must not meet the probability 0 of the others: it is taken out of the page, and a product of
-        // the places of NaN with the places that a row sees says where it belongs.
+        // A NaN counts for the rows that see it and must not meet the probability 0 of the others: it is taken out of the page, and a
+        // product of the places of NaN with the places that a row sees says where it belongs.
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           floatx4 hit[NQ];
@@ -356,8 +357,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
   }
 }
 
-// Joins the splits of the rows of a tile of ROWS, four rows at a time, `quads` times per block: each wave sums every fourth split, in their order,
-// then the waves' sums are added.  Lane: four columns of rows lane / 32 and 2 + lane / 32.
+// Joins the splits of the rows of a tile of ROWS, four rows at a time, `quads` times per block: each wave sums every fourth split, in their
+// order, then the waves' sums are added.  Lane: four columns of rows lane / 32 and 2 + lane / 32.
 template <int HD, int ROWS>
 __global__ __launch_bounds__(256) void attention_cached_join_kernel(const CachedArgs g, int quads) {
   constexpr int C = HD / 4;                        // lanes of a row
@@ -441,10 +442,10 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   p.rows = mean <= 16 ? 16 : mean <= 32 || head_dim < 64 ? 32 : 128;
   p.tiles = rows / p.rows + n_seqs;
   p.resident = 2 * compute_units();
-  // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (one token of a few
-  // sequences of up to 44 000: 24.9 us, 31.4 with 24), but no splits at all, and no second launch, up to 20 pages (four sequences of up to
-  // 1200: 14 us, 17.5 with splits of 8).  128 rows: 16 (931 + 238 + 16 + 17 tokens over 980, 314, 36 049 and 6026: 77 us, 88 with 8, 85 with 24;
-  // the other way 256 tokens over 4096 and over 1024: 49 us, 39 with 8).
+  // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (one
+  // token of a few sequences of up to 44 000: 24.9 us, 31.4 with 24), but no splits at all, and no second launch, up to 20 pages (four
+  // sequences of up to 1200: 14 us, 17.5 with splits of 8).  128 rows: 16 (931 + 238 + 16 + 17 tokens over 980, 314, 36 049 and 6026: 77
+  // us, 88 with 8, 85 with 24; the other way 256 tokens over 4096 and over 1024: 49 us, 39 with 8).
   p.least_pages = p.rows == 128 ? 16 : pages <= 20 ? 20 : 8;
   const int64_t whole = p.tiles * kv_heads;
   if (pages > p.least_pages) {

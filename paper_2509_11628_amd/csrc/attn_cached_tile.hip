@@ -1,20 +1,20 @@
 // Attention over 8-bit pages for many rows: the heads of a frame of new tokens.
 //
-// One block = 128 rows of one (sequence, key head), 4 waves x 32; a page of 64 keys is one tile.  A row is one query head of one new token.  The
-// four waves share a page through LDS, where it lies widened to bf16 (exactly: scales are powers of two), so each value is widened once per
-// 128 rows: the matrix instructions, not the conversions, are what is left.  The schedule is the one of the bf16 tiles without a cache: scores of
-// the next page under the exponentials of this one, pinned around every pair of matrix instructions.
+// One block = 128 rows of one (sequence, key head), 4 waves x 32; a page of 64 keys is one tile.  A row is one query head of one new token.
+// The four waves share a page through LDS, where it lies widened to bf16 (exactly: scales are powers of two), so each value is widened
+// once per 128 rows: the matrix instructions, not the conversions, are what is left.  The schedule is the one of the bf16 tiles without a
+// cache: scores of the next page under the exponentials of this one, pinned around every pair of matrix instructions.
 //
-// Bytes go to registers while the tile before is worked on and to LDS (two buffers each of keys and values) in the tile after, spread over its second
-// contraction.  Keys lie row-major, 16-byte chunks permuted as in the tiles without a cache.  Values arrive by dimension, as the page stores
-// them: 16 bytes are one dimension's keys of one lane group, in the order in which S^T hands them on.  Their two widened halves go to
-// place [half][tile of 16 dimensions][lane], so a fragment is one read of 16 bytes per lane, all lanes in a row.
+// Bytes go to registers while the tile before is worked on and to LDS (two buffers each of keys and values) in the tile after, spread over
+// its second contraction.  Keys lie row-major, 16-byte chunks permuted as in the tiles without a cache.  Values arrive by dimension, as the
+// page stores them: 16 bytes are one dimension's keys of one lane group, in the order in which S^T hands them on.  Their two widened halves
+// go to place [half][tile of 16 dimensions][lane], so a fragment is one read of 16 bytes per lane, all lanes in a row.
 //
-// What bounds it: the vector unit (exponentials, maxima, widening) and the LDS reads beside the matrix instructions, at two blocks per unit.  A frame of
-// 1590 tokens over 27 286, 24 heads of 128: 645 us, 826 TFLOP/s, 27 of it the join.  On the way there, us: widening in every wave's registers instead
-// (rows of 64 a wave) 1150; through LDS 950; without bank conflicts of the writes 745 with those of the values, 683 with those of the keys gone; without registers
-// that spill to memory, whose restores wait for the bytes on their way, 647 (three or four fragments ahead instead of two spill again: 650 and
-// 715; keys in units of 8 bytes, which spares the turn below, 802).
+// What bounds it: the vector unit (exponentials, maxima, widening) and the LDS reads beside the matrix instructions, at two blocks per
+// unit.  A frame of 1590 tokens over 27 286, 24 heads of 128: 645 us, 826 TFLOP/s, 27 of it the join.  On the way there, us: widening in
+// every wave's registers instead (rows of 64 a wave) 1150; through LDS 950; without bank conflicts of the writes 745 with those of the
+// values, 683 with those of the keys gone; without registers that spill to memory, whose restores wait for the bytes on their way, 647
+// (three or four fragments ahead instead of two spill again: 650 and 715; keys in units of 8 bytes, which spares the turn below, 802).
 #include <type_traits>
 
 #include "attn_cached.h"
@@ -35,8 +35,8 @@ __device__ inline int key_chunk(int c, int r) {
   return HD == 128 ? c ^ (r & 15) : HD == 64 ? c ^ (r & 7) ^ ((r >> 3) & 1) : c;
 }
 
-// Place of dimension l of lane group g among the 64 chunks of a value fragment: the 16 lanes {0-3, 12-15, 20-27} and so on that a read of 16 bytes takes
-// at a time hit different banks, and so do 8 threads that write four groups of two dimensions.
+// Place of dimension l of lane group g among the 64 chunks of a value fragment: the 16 lanes {0-3, 12-15, 20-27} and so on that a read of
+// 16 bytes takes at a time hit different banks, and so do 8 threads that write four groups of two dimensions.
 __device__ inline int value_place(int l, int g) { return g * 16 + (l ^ (2 * g)); }
 
 // a value that all lanes read, in a scalar register
@@ -93,8 +93,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     start = __builtin_amdgcn_readfirstlane(start);
     n = __builtin_amdgcn_readfirstlane(n);
     const int64_t r0 = static_cast<int64_t>(row_tile) * ROWS, rows = static_cast<int64_t>(n) * g.group;
-    int len = __builtin_amdgcn_readfirstlane(g.lens[f.seq]);
-    len = len < 0 ? 0 : min(len, g.max_len);
+    const int held = max(0, static_cast<int>(__builtin_amdgcn_readfirstlane(g.lens[f.seq]))), len = min(held, g.max_len);
 
     // rows 32 wave + 16 i + l16: token, head, number of keys that it sees
     auto place = [&](int i, int* tok, int64_t* column) {
@@ -104,7 +103,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     };
     int lim[2];
     const int last_tok = static_cast<int>((min(r0 + ROWS, rows) - 1) / g.group), first_tok = static_cast<int>(r0 / g.group);
-    const int most = g.causal ? max(0, len - n + last_tok + 1) : len, least = g.causal ? max(0, len - n + first_tok + 1) : len;
+    const int most = keys_of(g, held, len, n, last_tok), least = keys_of(g, held, len, n, first_tok);
     const int begin = split * f.each, end = min(begin + f.each, (most + PAGE - 1) / PAGE);
     const bool active = r0 + wave * 32 < rows;
 
@@ -114,7 +113,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
       int tok;
       int64_t column;
       place(i, &tok, &column);
-      lim[i] = g.causal ? max(0, len - n + tok + 1) : len;
+      lim[i] = keys_of(g, held, len, n, tok);
       const uint16_t* qp = g.q + (static_cast<int64_t>(start) + tok) * g.ldq + column;
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -132,8 +131,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
       }
     }
 
-    // Numbers of the unit's pages, 64 at a time, one a lane (lengths are bounded by the table's row).  One that is not held is worked on like the
-    // others, with some page's bytes, none of which any row sees.
+    // Numbers of the unit's pages, 64 at a time, one a lane (lengths are bounded by the table's row).  One that is not held is worked on
+    // like the others, with some page's bytes, none of which any row sees.
     const int32_t* table = g.table + static_cast<int64_t>(f.seq) * g.table_ld;
     const int tiles = end - begin;
     int ids = -1;
@@ -168,7 +167,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     };
     auto load_v = [&](int page) {
       const uint64_t at = static_cast<uint64_t>(page < 0 ? 0 : page) * heads;
-      vscale = scalar(reinterpret_cast<const float*>(vs_at + at * 4));
+      vscale = page < 0 ? 1.0f : scalar(reinterpret_cast<const float*>(vs_at + at * 4));      // (one that is no number would not leave the zeros zeros)
       const auto from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(v_at + at * (PAGE * HD)), 0, PAGE * HD, 0x00020000);
 #pragma unroll
       for (int u = 0; u < VU; ++u) va[u] = __builtin_amdgcn_raw_buffer_load_b128(from, tid * 16, 4096 * u, 0);
@@ -197,7 +196,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     // Whether some row does not see all of page `at` of the sequence, which is page `page` of the cache.
     auto is_edge = [&](int at, int page) { return (at + 1) * PAGE > least || page < 0; };
     // What is done once to the values of such a page: bytes past the last token, whatever they
-    // are, become 0, and so does a NaN, which must not meet the probability 0 of a row that does not see it.  The rows that do get it at the end.
+    // are, become 0, and so does a NaN, which must not meet the probability 0 of a row that does not see it.  The rows that do get it at
+    // the end.
     auto edge_v = [&](int at, int page) {
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
@@ -280,9 +280,9 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     SPECA_PIN();                                            \
   }
     constexpr int NS = 4 * KS, NV = 2 * DT, RA = 2, NP = 20;
-    // Tile in buffer `buf`, whose scores lie in sc with their reference known.  NEXT: its successor is page at1 of the sequence, page1 of the cache,
-    // whose keys lie in the other buffer and whose values are in va; page2 is the one behind it, whose keys are in ka, and page3 the one behind
-    // that.  (Where there is none, some page is loaded and staged, and not used.)
+    // Tile in buffer `buf`, whose scores lie in sc with their reference known.  NEXT: its successor is page at1 of the sequence, page1 of
+    // the cache, whose keys lie in the other buffer and whose values are in va; page2 is the one behind it, whose keys are in ka, and page3
+    // the one behind that.  (Where there is none, some page is loaded and staged, and not used.)
     auto tile = [&](floatx4 (&sc)[4][2], floatx4 (&sn)[4][2], int buf, int at1, int page1, int page2, int page3, auto next_tag) {
       constexpr bool NEXT = decltype(next_tag)::value;
       bf16x8 kf[NS], vf[NV], pf[2][2];

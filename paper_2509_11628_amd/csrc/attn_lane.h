@@ -1,5 +1,5 @@
-// What the attention kernels share at the level of a lane: packed conversions, exponentials, and the reductions over the lanes that hold one query
-// of a transposed 16x16 tile (l % 16, in the four groups l / 16).
+// What the attention kernels share at the level of a lane: packed conversions, exponentials, and the reductions over the lanes that hold
+// one query of a transposed 16x16 tile (l % 16, in the four groups l / 16).
 #pragma once
 
 #include "common.h"

@@ -115,9 +115,10 @@ __device__ __forceinline__ void buffer_to_lds(const uint16_t* buffer, int bytes,
 }
 
 // Rows of equal length (PLAIN), or packed sequences, of which causal tokens see themselves and those before them.
-// Packed, one MI355X: 5 sequences of 589 to 4608 tokens, 24 heads of 128: 605 to 640 us, 950 to 1010 TFLOP/s (power, as above); 12 causal ones of 19 to 4096, 32 heads over
-// 8 of 128: 334 to 345 us, 820 to 845 TFLOP/s of the products that count (a block's last two tiles are half hidden); 16 of 1 to 400 tokens, 16 heads of
-// 72: 17.5 us, a chain of waits (places, first tiles, up to 7 tiles), in which the keys of several heads a cache line go to one XCD.
+// Packed, one MI355X: 5 sequences of 589 to 4608 tokens, 24 heads of 128: 605 to 640 us, 950 to 1010 TFLOP/s (power, as above); 12 causal
+// ones of 19 to 4096, 32 heads over 8 of 128: 334 to 345 us, 820 to 845 TFLOP/s of the products that count (a block's last two tiles are
+// half hidden); 16 of 1 to 400 tokens, 16 heads of 72: 17.5 us, a chain of waits (places, first tiles, up to 7 tiles), in which the keys of
+// several heads a cache line go to one XCD.
 enum { PLAIN = 0, PACKED = 1, CAUSAL = 2 };
 struct TileArgs {
   const uint16_t *q, *k, *v;
@@ -158,9 +159,9 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
     head = pair - row * g.H;
     start = static_cast<int64_t>(row) * T;
   } else {
-    // Blocks b, b + 8, ... run on the same XCD.  The query heads of a key head go to one (prompts 377 -> 363 us), and where a head's row does not
-    // fill its cache lines, neighbouring key heads do.  Late tiles of causal sequences, the long ones, come first (13 sequences of up to 3008 tokens, 24
-    // heads of 64: 85 -> 68 us).
+    // Blocks b, b + 8, ... run on the same XCD.  The query heads of a key head go to one (prompts 377 -> 363 us), and where a head's row
+    // does not fill its cache lines, neighbouring key heads do.  Late tiles of causal sequences, the long ones, come first (13 sequences of
+    // up to 3008 tokens, 24 heads of 64: 85 -> 68 us).
     const int kv_heads = g.H / g.group, turn = blockIdx.x % g.H;
     const int each = kv_heads / 8, kv = HD % 64 == 0 || kv_heads % 8 ? turn % kv_heads : turn % 8 * each + turn / 8 % each;
     head = kv * g.group + turn / kv_heads;
@@ -303,8 +304,8 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
     for (int i = 0; i < 32; ++i)
       if (kt * 64 + (i >> 3) * 16 + 4 * g4 + (i & 3) > last_key((i >> 2) & 1)) s[i >> 3][(i >> 2) & 1][i & 3] = -INFINITY;
   };
-  // A value that is no number must not meet the probability 0 of a causal query that does not see it: in the tile that a wave's queries see in
-  // part, where there is one, it counts as 0 in the product, and for the queries that see it is added here.
+  // A value that is no number must not meet the probability 0 of a causal query that does not see it: in the tile that a wave's queries see
+  // in part, where there is one, it counts as 0 in the product, and for the queries that see it is added here.
   auto add_odd = [&](int from, int to) {                           // of keys from .. to - 1
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)

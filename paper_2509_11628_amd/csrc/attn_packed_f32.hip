@@ -1,13 +1,13 @@
 // Attention of packed sequences on the fp32 matrix instructions: fp32 tensors, and bf16 ones that the bf16 kernel does not take.
 //
-// One block = 16 QT queries of one (sequence, head); its four waves take the 16-key tiles w, w + 4, ... with an online softmax of their own and
-// merge at the end.  Transposed products: S^T[key][query] leaves lane l with keys 4 (l / 16) .. + 3 of query l % 16, which is the second
-// operand of the O^T product as it stands (instruction r takes keys 4 q + r).  The head dimension is dealt to the 16-row tiles of O^T in pieces
-// of four (tile i % 4 of group i / 4 owns dimensions 64 g + 4 row + i), so a lane's values are 16-byte pieces of V and of the output.
-// T = storage type of q, k, v and the output; arithmetic is fp32.
+// One block = 16 QT queries of one (sequence, head); its four waves take the 16-key tiles w, w + 4, ... with an online softmax of their own
+// and merge at the end.  Transposed products: S^T[key][query] leaves lane l with keys 4 (l / 16) .. + 3 of query l % 16, which is the
+// second operand of the O^T product as it stands (instruction r takes keys 4 q + r).  The head dimension is dealt to the 16-row tiles of
+// O^T in pieces of four (tile i % 4 of group i / 4 owns dimensions 64 g + 4 row + i), so a lane's values are 16-byte pieces of V and of the
+// output. T = storage type of q, k, v and the output; arithmetic is fp32.
 //
-// What bounds it: fragments straight from memory (16 rows x 64 bytes per load), of which a unit takes 33 to 34 bytes per ns.  Sequences of 1024, 77, 777 and 256
-// tokens, 6 heads of 64: 38 us, 69 TFLOP/s; with 32 queries a block 44, for want of blocks.
+// What bounds it: fragments straight from memory (16 rows x 64 bytes per load), of which a unit takes 33 to 34 bytes per ns.  Sequences of
+// 1024, 77, 777 and 256 tokens, 6 heads of 64: 38 us, 69 TFLOP/s; with 32 queries a block 44, for want of blocks.
 #include "attn_lane.h"
 #include "operators.h"
 

@@ -4,8 +4,9 @@
 // of amax: 448 = 1.75 * 2^8, so e = exponent(amax) - 8, and one more where the mantissa is above 1.75.
 //
 // A page and head is one block's, for keys and for values each: amax needs all of its new tokens, and the bytes that stay need the old scale.
-// Bound by memory and by the chain of waits of one block (place, tokens, maximum, bytes).  Storing 2512 tokens of 24 heads of 128 in bf16 takes 16 us, loading them
-// back 12 (45 MB each way); 16 single tokens of 8 heads 6 and 4.  One value per thread at a time took 51 and 30, 14 and 12.
+// Bound by memory and by the chain of waits of one block (place, tokens, maximum, bytes).  Storing 2512 tokens of 24 heads of 128 in bf16
+// takes 16 us, loading them back 12 (45 MB each way); 16 single tokens of 8 heads 6 and 4.  One value per thread at a time took 51 and 30,
+// 14 and 12.
 #include "operators.h"
 
 namespace speca {
@@ -63,8 +64,8 @@ __device__ inline int scale_exponent(uint32_t amax_bits) {          // of a fini
   const int e = static_cast<int>(amax_bits >> 23) - 127 - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
   return amax_bits == 0 || e < kLowest ? kLowest : e > kHighest ? kHighest : e;
 }
-// Four values to e4m3, nearest even; they are scaled already.  The conversion makes NaN of what lies beyond 448, so that is cut off first; NaN
-// passes the comparisons.
+// Four values to e4m3, nearest even; they are scaled already.  The conversion makes NaN of what lies beyond 448, so that is cut off first;
+// NaN passes the comparisons.
 __device__ inline float cut(float v) { return v > 448.0f ? 448.0f : v < -448.0f ? -448.0f : v; }
 __device__ inline uint32_t encode4(float a, float b, float c, float d) {
   const int low = __builtin_amdgcn_cvt_pk_fp8_f32(cut(a), cut(b), 0, false);
@@ -119,7 +120,8 @@ __device__ inline Place find_place(const Args& g, int tile) {
 }
 
 // One block: the keys (blockIdx.y == 0) or values of one head of one page.  A thread has four consecutive tokens of eight features, which are
-// four consecutive bytes of eight rows of a value page; threads next to each other go along the page's rows (features of keys, tokens of values).
+// four consecutive bytes of eight rows of a value page; threads next to each other go along the page's rows (features of keys, tokens of
+// values).
 struct Unit {
   int t, d;                         // first token of the page, first feature
   bool live;

@@ -2,10 +2,10 @@
 //
 //   y = x / sqrt(mean(x^2) + eps) * w      (a, b) -> (a cos - b sin, a sin + b cos),  angle = position[axis] * rate[pair]
 //
-// Bound by memory: every value is read and written once, at 6 operations.  27 286 tokens of 24 + 24 heads of 128 with norm: 140 us, 4.8 TB/s (a large copy moves
-// 5.0).  What is not memory is the angle: position x rate is formed in 64 bits and in turns, of which only the fraction counts, so a position
-// of 10^6 keeps an angle of 10^-9; the lanes that hold the same pairs of several heads share the work on it (184 us before that and before
-// the token's addresses were scalar).
+// Bound by memory: every value is read and written once, at 6 operations.  27 286 tokens of 24 + 24 heads of 128 with norm: 140 us, 4.8
+// TB/s (a large copy moves 5.0).  What is not memory is the angle: position x rate is formed in 64 bits and in turns, of which only the
+// fraction counts, so a position of 10^6 keeps an angle of 10^-9; the lanes that hold the same pairs of several heads share the work on it
+// (184 us before that and before the token's addresses were scalar).
 #include <algorithm>
 #include <cmath>
 
@@ -83,9 +83,9 @@ __device__ inline void rope_store(T* p, uint32_t lo, uint32_t hi, const float (&
   rope_write<VP>(p + (HALVES || VP == 1 ? hi : lo + VP), b);
 }
 
-// One wave = one token and some of its heads, steps of 64 / lanes_per_head heads of q, then of k; a lane owns VP pairs of a head.  Its pieces are
-// VP features at lo and VP at hi: with HALVES the two sides of its pairs, otherwise neighbours, of which features 2j and 2j + 1 are a pair.
-// What belongs to the token or the step is in scalar registers, so a lane's addresses are one offset each.
+// One wave = one token and some of its heads, steps of 64 / lanes_per_head heads of q, then of k; a lane owns VP pairs of a head.  Its
+// pieces are VP features at lo and VP at hi: with HALVES the two sides of its pairs, otherwise neighbours, of which features 2j and 2j + 1
+// are a pair. What belongs to the token or the step is in scalar registers, so a lane's addresses are one offset each.
 template <typename T, int VP, bool HALVES, bool NORM>
 __global__ __launch_bounds__(256) void rope_axes_kernel(const RopeArgs g) {
   constexpr int UN = 4;
@@ -283,7 +283,8 @@ Error launch_rope_axes(int dtype, const speca_rope& rope, const int32_t* positio
     }
   }
   // Four pairs a lane where every piece of four features lies at a whole piece (16 bytes in fp32, 8 in bf16), one pair otherwise (140
-  // and 620 us for 27 286 tokens of 48 heads of 128).  With HALVES the pairs of a lane must end with the rotation, and what does not turn has to be whole lanes too.
+  // and 620 us for 27 286 tokens of 48 heads of 128).  With HALVES the pairs of a lane must end with the rotation, and what does not turn
+  // has to be whole lanes too.
   const size_t piece = 4 * dtype_size(dtype);
   uintptr_t at = 0;
   for (const RopeSide& s : g.side)

@@ -469,6 +469,112 @@ def test_cached_scores_without_a_maximum():
     assert torch.equal(got[0], clean[0]) and bool(got[1].isnan().all())
 
 
+@pytest.mark.parametrize("hd", [64, 72, 128])
+@pytest.mark.parametrize("H,tokens", [(4, 1), (4, 12), (8, 40)])
+def test_cached_many_sequences(hd, H, tokens):
+    """More sequences than a wave has lanes, long and short ones, with and without new tokens, in every height of tiles."""
+    bd = _bd()
+    rng = np.random.default_rng(tokens)
+    lens = [int(n) for n in rng.integers(0, 200, 150)]
+    lens[70], lens[149] = 6000, 2500
+    new = [0 if s % 11 == 3 else int(rng.integers(1, 2 * tokens + 1)) if s % 5 else tokens for s in range(150)]
+    _cached_check(bd, new, lens, H, 2, hd, True, seed=5)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_cached_one_and_many_tokens_in_one_call(hd):
+    """Single tokens beside a whole prompt, and empty sequences alone."""
+    bd = _bd()
+    _cached_check(bd, [1, 700, 1, 0], [2000, 700, 65, 10], 4, 2, hd, True)
+    _cached_check(bd, [0, 0], [100, 0], 4, 2, hd, True)
+
+
+@pytest.mark.parametrize("hd", [64, 72, 128])
+@pytest.mark.parametrize("new", [2, 20, 200])
+def test_cached_pages_that_are_none(hd, new):
+    """Pages that are not held inside, at the start and at the end of a range, and more tokens than the table has room for, for every height
+    of tiles; page 0, which belongs to nobody, holds NaN and so do its scales."""
+    bd = _bd()
+    Hkv, H, n = 1, 2, 40 * 64 + 90
+    cache, table, _ = _fill(bd, [n, 64], Hkv, hd)
+    table = table[:1].copy()
+    table[0, [0, 5, 6, 7, 17, 39]] = [-1, 10 ** 6, cache.k.shape[0], -7, -2 ** 31, 2 ** 31 - 1]
+    table = table[:, :40]
+    free = [p for p in range(cache.k.shape[0]) if p not in table[0]]
+    if 0 not in free:                                    # page 0 gives its place to a free one
+        p = free[0]
+        for t in (cache.k, cache.v, cache.k_scale, cache.v_scale):
+            t[p] = t[0].clone()
+        table[0, table[0] == 0] = p
+    cache.k[0], cache.v[0] = 0x7F, 0xFF
+    cache.k_scale[0], cache.v_scale[0] = math.nan, math.inf
+    twin = ref.Cache(cache)
+    q = ref.randn((new, H, hd), torch.bfloat16, 3)
+    (k, held), (v, _) = twin.values(0, table[0], n), twin.values(1, table[0], n)
+    assert not bool(held.all())
+    for causal in (False, True):
+        got = bd.attention_cached(q, ref.starts_of([new]), cache, _dev(table), _dev([n]), causal=causal)
+        sees = held[None].expand(new, n)
+        if causal:
+            sees = sees & (torch.arange(n, device="cuda")[None] <= n - new + torch.arange(new, device="cuda")[:, None])
+        ref.close(got, *ref.attention(q, k, v, sees, 1.0 / math.sqrt(hd), BF16_P, torch.bfloat16))
+
+
+@pytest.mark.parametrize("hd", [64, 72, 128])
+@pytest.mark.parametrize("new", [5, 90])
+def test_cached_nan_in_a_split_range(hd, new):
+    """A NaN among the values of a long sequence reaches every row that sees it, whichever split holds it, and no other feature."""
+    bd = _bd()
+    H, Hkv, n = 4, 2, 5000
+    cache, table, _ = _fill(bd, [n], Hkv, hd)
+    q = ref.randn((new, H, hd), torch.bfloat16, 9)
+    run = lambda: bd.attention_cached(q, ref.starts_of([new]), cache, _dev(table), _dev([n]), causal=True)  # noqa: E731
+    clean = run()
+    for at in (0, 2222, n - new, n - 1):
+        page, place = int(table[0, at // 64]), ref.PLACE[at % 64]
+        old = cache.v.clone()
+        cache.v[page, 1, 7, place] = 0x7F
+        got = run()
+        cache.v.copy_(old)
+        see = max(0, at - (n - new))                     # the first new token that sees it
+        assert torch.equal(got[:see], clean[:see]) and torch.equal(got[:, :2], clean[:, :2])
+        assert bool(got[see:, 2:, 7].isnan().all()) and torch.equal(got[..., 8:], clean[..., 8:]) and torch.equal(got[..., :7], clean[..., :7])
+
+
+def test_cached_offsets_that_are_none():
+    """Offsets that fall or leave the buffer reach nothing outside it."""
+    bd = _bd()
+    cache, table, _ = _fill(bd, [3000, 100, 64, 7, 900], 2, 64)
+    pool = torch.full((120, 4, 64), 5.0, dtype=torch.bfloat16, device="cuda")
+    q = ref.randn((100, 4, 64), torch.bfloat16, 1)
+    for starts in ([0, 40, 10, 300, -5, 7], [90, 2 ** 31 - 1, -2 ** 31, 100, 0, 100]):
+        bd.attention_cached(q, _dev(starts), cache, _dev(table), _dev([3000, 100, 64, 7, 900]), out=pool[10:110])
+        assert bool((pool[:10] == 5.0).all()) and bool((pool[110:] == 5.0).all())
+
+
+def test_cache_beyond_32_bits():
+    """Pages whose bytes lie more than 2^32 behind the first, in every call."""
+    bd = _bd()
+    heads, hd, pages = 8, 128, 66000                    # 4.3 GB of keys and as much of values
+    cache = bd.KVCache.empty(pages, heads, hd)
+    near = bd.KVCache.empty(8, heads, hd)
+    far, close = [pages - 1, 65999 - 7, 65537], [0, 3, 5]
+    n = 150
+    k, v = ref.randn((n, heads, hd), torch.bfloat16, 1), ref.randn((n, heads, hd), torch.bfloat16, 2)
+    got = []
+    for c, t in ((cache, far), (near, close)):
+        table = _dev([t])
+        bd.kv_store(c, table, _dev([0]), k, v, ref.starts_of([n]))
+        out = [*bd.kv_load(c, table, _dev([0]), ref.starts_of([n]), n, torch.bfloat16)]
+        for new in (1, 40, 140):
+            q = ref.randn((new, 8, hd), torch.bfloat16, 3)
+            out.append(bd.attention_cached(q, ref.starts_of([new]), c, table, _dev([n])))
+        got.append(out)
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert float((got[0][0] - k).abs().max()) <= 2.0 ** -4 * float(k.abs().max())
+
+
 # ---- together -----------------------------------------------------------------------------------------------
 
 
@@ -544,6 +650,26 @@ def test_on_another_stream():
     s.synchronize()
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """Two chains with caches of their own, in turn on two streams without a wait between."""
+    bd = _bd()
+    chains = [_chain(bd) for _ in range(2)]
+    chains[1][0].copy_(ref.randn(tuple(chains[1][0].shape), torch.bfloat16, 77))
+    want = [run() for _, run in chains]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in chains]
+    for turn in range(8):
+        got = []
+        for (_, run), s in zip(chains, streams):
+            with torch.cuda.stream(s):
+                got.append(run())
+        for s in streams:
+            s.synchronize()
+        for a, b in zip(want, got):
+            for x, y in zip(a, b):
+                assert torch.equal(x, y), turn
 
 
 def test_captured_and_replayed():
