@@ -45,14 +45,18 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, g4 = lane >> 4;
   const Deal d = deal<ROWS>(g);
-  if (g.shares && blockIdx.x == 0 && wave == 0) find_unit<ROWS>(g, d, 0, g.shares);
+  if (g.shares && blockIdx.x == 0 && wave == 0) {
+    Place all;
+    find_unit<ROWS>(g, d, 0, g.shares, &all);
+  }
   // Blocks b, b + 8, ... run on the same XCD: a round of the grid gives each XCD a run of units, which share keys where rows are many.
   const int per_xcd = gridDim.x / 8;
+  Place search;
   for (int64_t round = 0;; ++round) {
     const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (round * gridDim.x >= d.units) break;
     if (unit >= d.units) continue;
-    const Found f = find_unit<ROWS>(g, d, unit, nullptr);
+    const Found f = find_unit<ROWS>(g, d, unit, nullptr, &search);
     if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;        // (offsets that overlap: there is no room for their sums)
     const int tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits, seq = f.seq;
     int start, n;

@@ -85,7 +85,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
   for (int64_t round = 0; round * gridDim.x < deal_.units; ++round) {
     const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
     if (unit >= deal_.units) continue;
-    const Found f = find_unit<ROWS>(g, deal_, unit, nullptr);
+    Place search;                             // (kept from one unit to the next, it costs more registers than it saves time)
+    const Found f = find_unit<ROWS>(g, deal_, unit, nullptr, &search);
     if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;      // (offsets that overlap: there is no room for their sums)
     const int row_tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits;
     int start, n;
@@ -167,7 +168,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     };
     auto load_v = [&](int page) {
       const uint64_t at = static_cast<uint64_t>(page < 0 ? 0 : page) * heads;
-      vscale = page < 0 ? 1.0f : scalar(reinterpret_cast<const float*>(vs_at + at * 4));      // (one that is no number would not leave the zeros zeros)
+      vscale = scalar(reinterpret_cast<const float*>(vs_at + at * 4));
       const auto from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint8_t*>(v_at + at * (PAGE * HD)), 0, PAGE * HD, 0x00020000);
 #pragma unroll
       for (int u = 0; u < VU; ++u) va[u] = __builtin_amdgcn_raw_buffer_load_b128(from, tid * 16, 4096 * u, 0);
@@ -199,6 +200,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
     // are, become 0, and so does a NaN, which must not meet the probability 0 of a row that does not see it.  The rows that do get it at
     // the end.
     auto edge_v = [&](int at, int page) {
+      if (page < 0) vscale = 1.0f;            // (a scale that is no number would not leave the zeros zeros)
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
         const int left = (page < 0 ? 0 : len) - (at * PAGE + 4 * (tid & 3));
@@ -477,7 +479,10 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
       }
     }
   }
-  if (g.shares && blockIdx.x == 0 && wave == 0) find_unit<ROWS>(g, deal_, 0, g.shares);
+  if (g.shares && blockIdx.x == 0 && wave == 0) {
+    Place all;
+    find_unit<ROWS>(g, deal_, 0, g.shares, &all);
+  }
 }
 
 }  // namespace

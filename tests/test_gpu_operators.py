@@ -201,6 +201,32 @@ def test_packed_matches_plain_attention_of_equal_lengths():
     assert float((got.double() - want).abs().max()) <= 2 * 2.0 ** -8 * float(flat[:, 2].abs().max()) * 2
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_beyond_32_bits(dtype):
+    """Tokens whose elements lie more than 2^32 bytes behind the first, in attention and in the rotation."""
+    bd = _bd()
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    total, H, hd, lens = 290_000, 64, 128, [130, 70]
+    n = sum(lens)
+    q, k, v = (torch.empty((total, H, hd), dtype=dt, device="cuda") for _ in range(3))
+    for i, x in enumerate((q, k, v)):
+        x[-n:] = ref.randn((n, H, hd), dt, i)
+    assert (total - n) * H * hd * q.element_size() > 2 ** 32
+    for causal in (False, True):
+        got = bd.attention_packed(q, k, v, ref.starts_of(lens, total - n), causal=causal)
+        at = total - n
+        for m in lens:
+            sees = torch.ones((m, m), dtype=torch.bool, device="cuda")
+            x = [t[at:at + m] for t in (q, k, v)]
+            ref.close(got[at:at + m], *ref.attention(*x, sees.tril() if causal else sees, hd ** -0.5, BF16_P if dtype == "bf16" else 0.0, dt))
+            at += m
+    rope, pos = bd.make_rope((64, 64)), torch.arange(2 * total, dtype=torch.int32, device="cuda").view(total, 2)
+    q[:-n] = 1.0
+    want = bd.rope_axes(rope, pos[-n:].clone(), q[-n:].clone())
+    bd.rope_axes(rope, pos, q, out=q)
+    assert torch.equal(q[-n:], want)
+
+
 # ---- the cache ----------------------------------------------------------------------------------------------
 
 
@@ -695,3 +721,40 @@ def test_captured_and_replayed():
             torch.cuda.synchronize()
             for a, b in zip(want, out):
                 assert torch.equal(a, b), turn
+
+
+def test_captured_step_replayed_over_growing_sequences():
+    """One graph of a step of single tokens, replayed while the lists on the device grow past page ends: each time the bits of an eager step."""
+    bd = _bd()
+    H, Hkv, hd, n = 8, 2, 128, 3
+    table = _dev(_tables(60, [20, 20, 20], 20))
+    lens = [62, 0, 1150]
+    caches = [bd.KVCache.empty(60, Hkv, hd) for _ in range(2)]
+    k, v = ref.randn((sum(lens), Hkv, hd), torch.bfloat16, 1), ref.randn((sum(lens), Hkv, hd), torch.bfloat16, 2)
+    for c in caches:
+        bd.kv_store(c, table, _dev([0] * n), k, v, ref.starts_of(lens))
+    x = ref.randn((n, H + 2 * Hkv, hd), torch.bfloat16, 3)
+    starts, past, held = ref.starts_of([1] * n), _dev(lens), _dev(lens) + 1
+    pos = past[:, None].clone()
+    rope = bd.make_rope((hd,), pairing=bd.ROPE_HALVES)
+
+    def step(cache):
+        q, kk = bd.rope_axes(rope, pos, x[:, :H], x[:, H:H + Hkv])
+        bd.kv_store(cache, table, past, kk, x[:, H + Hkv:], starts)
+        return bd.attention_cached(q, starts, cache, table, held)
+    scratch = bd.KVCache.empty(60, Hkv, hd)
+    step(scratch)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step(caches[0])
+    for turn in range(6):
+        x.copy_(ref.randn(tuple(x.shape), torch.bfloat16, 10 + turn))
+        want = step(caches[1])
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and not bool(out.isnan().any()), turn
+        for a, b in zip((caches[0].k, caches[0].v, caches[0].k_scale, caches[0].v_scale), (caches[1].k, caches[1].v, caches[1].k_scale, caches[1].v_scale)):
+            assert torch.equal(a, b), turn
+        for t in (past, held, pos):
+            t += 1
