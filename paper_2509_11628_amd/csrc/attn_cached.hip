@@ -363,13 +363,13 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
 
 // Joins the splits of the rows of a tile of ROWS, four rows at a time, `quads` times per block: each wave sums every fourth split, in their
 // order, then the waves' sums are added.  Lane: four columns of rows lane / 32 and 2 + lane / 32.
-template <int HD, int ROWS>
-__global__ __launch_bounds__(256) void attention_cached_join_kernel(const CachedArgs g, int quads) {
+template <int HD, int ROWS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void attention_cached_join_kernel(const CachedArgs g, int quads) {
   constexpr int C = HD / 4;                        // lanes of a row
   static_assert(C <= 32, "two rows a wave");
-  __shared__ float tops[4][4];
-  __shared__ __align__(16) floatx4 sums[4][4][C];
-  __shared__ float totals[4][4];
+  __shared__ float tops[WAVES][4];
+  __shared__ __align__(16) floatx4 sums[WAVES][4][C];
+  __shared__ float totals[WAVES][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int parts = ROWS / 4 / quads, part = blockIdx.x % parts, rest = blockIdx.x / parts, head = rest % g.kv_heads, tile = rest / g.kv_heads;
   const int seq = packed_find(g.seqs, tile, g.group, ROWS, 0);
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
     auto stat = [&](int s, int which, int r) { return g.stats[((first + static_cast<int64_t>(s) * f.tiles) * 2 + which) * ROWS + quad * 4 + r]; };
 
     float top = -INFINITY;                           // of row lane % 4, over the splits of this lane, then of all
-    for (int s = tid >> 2; s < f.splits; s += 64) top = fmaxf(top, stat(s, 0, tid & 3));
+    for (int s = tid >> 2; s < f.splits; s += 16 * WAVES) top = fmaxf(top, stat(s, 0, tid & 3));
     for (int off = 4; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
     if (lane < 4) tops[wave][lane] = top;
     __syncthreads();
@@ -394,11 +394,13 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const int r = 2 * half + (lane >> 5);
-      m[half] = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+      m[half] = tops[0][r];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) m[half] = fmaxf(m[half], tops[w][r]);
       off[half] = m[half] == -INFINITY ? 0.0f : m[half] * g.scale_log2e;
     }
 #pragma unroll 8
-    for (int s = wave; s < f.splits; s += 4)
+    for (int s = wave; s < f.splits; s += WAVES)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int r = 2 * half + (lane >> 5);
@@ -418,8 +420,13 @@ __global__ __launch_bounds__(256) void attention_cached_join_kernel(const Cached
     __syncthreads();
     const int r = tid / C, c = tid - r * C;
     if (tid < 4 * C && r0 + quad * 4 + r < rows) {
-      const floatx4 v = (sums[0][r][c] + sums[1][r][c]) + (sums[2][r][c] + sums[3][r][c]);
-      const float total = (totals[0][r] + totals[1][r]) + (totals[2][r] + totals[3][r]);
+      floatx4 v = sums[0][r][c];
+      float total = totals[0][r];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) {
+        v += sums[w][r][c];
+        total += totals[w][r];
+      }
       const int64_t row = r0 + quad * 4 + r;
       const int tok = static_cast<int>(row / g.group), sub = static_cast<int>(row - static_cast<int64_t>(tok) * g.group);
       uint16_t* op = g.out + (static_cast<int64_t>(start) + tok) * g.ldo + (static_cast<int64_t>(head) * g.group + sub) * HD + 4 * c;
@@ -468,7 +475,9 @@ void launch_join(const CachedArgs& g, const Plan& p, hipStream_t st) {
   // a block per four rows while that leaves the chip room, else one per 32
   const int64_t quads = p.tiles * g.kv_heads * (ROWS / 4);
   const int each = quads > 8 * p.resident ? (ROWS / 4 < 8 ? ROWS / 4 : 8) : 1;
-  attention_cached_join_kernel<HD, ROWS><<<static_cast<unsigned>(quads / each), 256, 0, st>>>(g, each);
+  const unsigned blocks = static_cast<unsigned>(quads / each);
+  if (quads <= p.resident) attention_cached_join_kernel<HD, ROWS, 16><<<blocks, 1024, 0, st>>>(g, each);
+  else attention_cached_join_kernel<HD, ROWS, 4><<<blocks, 256, 0, st>>>(g, each);
 }
 template <int HD>
 void launch_hd(const CachedArgs& g, const Plan& p, hipStream_t st) {
