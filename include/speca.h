@@ -256,21 +256,21 @@ int speca_attention(void* hip_stream, int dtype, const void* qkv, void* out, int
 /* ---- attention of packed and cached sequences, callable on its own --------------------------- */
 
 /* Common to the five calls below.  Tensors are DEVICE memory; a token's heads lie one after the other ([heads][head_dim]
- * without gaps) and tokens are ld elements apart, so q, k and v may be views of one layer's output [tokens][(H + 2 Hkv) head_dim].
- * Query head h reads key and value head h / (heads / kv_heads); heads must be a multiple of kv_heads.
- * Sequences of different lengths are laid end to end: sequence s holds tokens starts[s] .. starts[s + 1] - 1 of a buffer of `total`
- * tokens (starts: DEVICE int32 [n_seqs + 1], rising; a sequence may be empty).  Tokens below starts[0] and from starts[n_seqs] on
- * are neither read nor written.  Offsets are clamped to 0 .. total, so none reads or writes outside the buffers.
- * Everything is asynchronous on hip_stream, whose device must be the current one; nothing is allocated, kept or synchronised, so calls may be captured
- * into a HIP graph.  No tokens (total = 0) is no work.  Errors: message via speca_last_error(NULL).  Results do not depend on
- * timing: the same inputs give the same bits. */
+ * without gaps) and tokens are ld elements apart, so q, k and v may be views of one layer's output [tokens][(H + 2 Hkv)
+ * head_dim]. Query head h reads key and value head h / (heads / kv_heads); heads must be a multiple of kv_heads. Sequences of
+ * different lengths are laid end to end: sequence s holds tokens starts[s] .. starts[s + 1] - 1 of a buffer of `total` tokens
+ * (starts: DEVICE int32 [n_seqs + 1], rising; a sequence may be empty).  Tokens below starts[0] and from starts[n_seqs] on are
+ * neither read nor written.  Offsets are clamped to 0 .. total, so none reads or writes outside the buffers. Everything is
+ * asynchronous on hip_stream, whose device must be the current one; nothing is allocated, kept or synchronised, so calls may be
+ * captured into a HIP graph.  No tokens (total = 0) is no work.  Errors: message via speca_last_error(NULL).  Results do not
+ * depend on timing: the same inputs give the same bits. */
 
 enum { SPECA_ROPE_ADJACENT = 0, SPECA_ROPE_HALVES = 1 };
 enum { SPECA_ROPE_PER_AXIS = 0, SPECA_ROPE_JOINT = 1 };
 #define SPECA_ROPE_MAX_AXES 4
 /* Rotary positions with several axes (time, height, width).  R = sum of dims features of a head turn in R / 2 pairs; the features
- * from R on stay.  Pair i is features (2i, 2i + 1) (ADJACENT) or (i, i + R / 2) (HALVES).  The first dims[0] / 2 pairs turn with the
- * first axis, the next dims[1] / 2 with the second, ...: pair j of axis a by
+ * from R on stay.  Pair i is features (2i, 2i + 1) (ADJACENT) or (i, i + R / 2) (HALVES).  The first dims[0] / 2 pairs turn with
+ * the first axis, the next dims[1] / 2 with the second, ...: pair j of axis a by
  *   position[a] * scale[a] * theta[a]^(-2 j / dims[a])        (PER_AXIS: every axis has its own spectrum)
  *   position[a] * scale[a] * theta[0]^(-2 i / R)              (JOINT: one spectrum over all pairs, i = pair of the head)
  * radians, formed in 64 bits, so far positions keep their angle. */
@@ -296,10 +296,10 @@ int speca_rope_axes(void* hip_stream, int dtype, const speca_rope* rope, const i
                     float eps, const speca_rope_io* q, const speca_rope_io* k);
 
 /* out = softmax(scale q k^T) v inside every sequence; causal != 0: a token sees itself and the tokens before it.
- * scale 0 = 1 / sqrt(head_dim).  out: [total][heads][head_dim], tokens ldo apart; may not overlap the inputs.  head_dim 16, 32, 64, 72 or 128.  What a
- * token does not see has no part in its result, whatever it holds (infinities and NaN included).  bf16 runs on the bf16 matrix instructions where
- * head_dim is 64, 72 or 128, q, k and v are 16-byte aligned with distances of whole 16 bytes (below 2^23 elements for k and v), out 8-byte; on the
- * fp32 ones, five to ten times slower, elsewhere. */
+ * scale 0 = 1 / sqrt(head_dim).  out: [total][heads][head_dim], tokens ldo apart; may not overlap the inputs.  head_dim 16, 32,
+ * 64, 72 or 128.  What a token does not see has no part in its result, whatever it holds (infinities and NaN included).  bf16
+ * runs on the bf16 matrix instructions where head_dim is 64, 72 or 128, q, k and v are 16-byte aligned with distances of whole 16
+ * bytes (below 2^23 elements for k and v), out 8-byte; on the fp32 ones, five to ten times slower, elsewhere. */
 int speca_attention_packed(void* hip_stream, int dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                            void* out, int64_t ldo, const int32_t* starts, int n_seqs, int total, int heads, int kv_heads, int head_dim,
                            int causal, float scale);
@@ -310,10 +310,10 @@ int speca_attention_packed(void* hip_stream, int dtype, const void* q, int64_t l
  *            what one lane of a matrix instruction reads is then 16 bytes in one piece
  *   k_scale, v_scale  float [pages][kv_heads]
  * A byte is e4m3 (OCP: largest 448, 0x7F and 0xFF are NaN) and stands for its value x the scale of its page and head, a power of
- * two 2^e with -100 <= e <= 119, the smallest whose 448-fold reaches every finite value that was stored in the page (or larger, where
- * larger tokens have been overwritten).  With powers of two, bytes times scale are exact in bf16, and a page that grows keeps its tokens'
- * values when a larger token takes the scale up, unless they become subnormal (below scale / 64; then rounded once more).
- * k and v must be 16-byte aligned.  head_dim 16, 32, 64, 72 or 128. */
+ * two 2^e with -100 <= e <= 119, the smallest whose 448-fold reaches every finite value that was stored in the page (or larger,
+ * where larger tokens have been overwritten).  With powers of two, bytes times scale are exact in bf16, and a page that grows
+ * keeps its tokens' values when a larger token takes the scale up, unless they become subnormal (below scale / 64; then rounded
+ * once more). k and v must be 16-byte aligned.  head_dim 16, 32, 64, 72 or 128. */
 #define SPECA_KV_PAGE 64
 typedef struct speca_kv_cache {
   void* k;
@@ -330,8 +330,8 @@ typedef struct speca_kv_table {
 } speca_kv_table;
 
 /* Tokens of the packed k and v ([total][kv_heads][head_dim] of type dtype) become tokens past[s], past[s] + 1, ... of sequence s (past: DEVICE
- * int32 [n_seqs], >= 0).  Rounding to nearest, ties to even; infinities saturate, NaN stays.  Tokens of a page below past[s] are kept, what lay from the last new token
- * on in its page is cleared.  Two sequences of one call must not write the same page. */
+ * int32 [n_seqs], >= 0).  Rounding to nearest, ties to even; infinities saturate, NaN stays.  Tokens of a page below past[s] are
+ * kept, what lay from the last new token on in its page is cleared.  Two sequences of one call must not write the same page. */
 int speca_kv_store(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* past,
                    const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total);
 /* The other way round: tokens first[s], first[s] + 1, ... of sequence s, as the values they stand for, into packed k and v.  (In both calls a run
@@ -340,11 +340,12 @@ int speca_kv_load(void* hip_stream, int dtype, const speca_kv_cache* cache, cons
                   void* k, int64_t ldk, void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total);
 
 /* Attention of the new tokens q ([total][heads][head_dim], bf16) over the first lens[s] tokens of their sequence in the cache
- * (lens: DEVICE int32 [n_seqs]; the new tokens' own keys are among them if they were stored).  causal != 0: of n new tokens the i-th sees tokens 0 .. lens[s] - n + i.
- * A token that sees nothing (lens[s] = 0, or causal with more new tokens than held) gives 0.  max_len: no sequence is longer (tokens from there
- * on are not attended to); it sets how the work is split, as n_seqs and total do.  out: bf16, tokens ldo apart.
- * dtype: SPECA_BF16 (SPECA_F32 is SPECA_EUNSUPPORTED).  workspace: DEVICE, 16-byte aligned, of at least
- * speca_attention_cached_workspace bytes, in use until the call's work has ended; calls that may overlap need one each. */
+ * (lens: DEVICE int32 [n_seqs]; the new tokens' own keys are among them if they were stored).  causal != 0: of n new tokens the
+ * i-th sees tokens 0 .. lens[s] - n + i. A token that sees nothing (lens[s] = 0, or causal with more new tokens than held) gives
+ * 0.  max_len: no sequence is longer (tokens from there on are not attended to); it sets how the work is split, as n_seqs and
+ * total do.  out: bf16, tokens ldo apart; may not overlap q. dtype: SPECA_BF16 (SPECA_F32 is SPECA_EUNSUPPORTED).  workspace:
+ * DEVICE, 16-byte aligned, of at least speca_attention_cached_workspace bytes, in use until the call's work has ended; calls that
+ * may overlap need one each. */
 int speca_attention_cached(void* hip_stream, int dtype, const void* q, int64_t ldq, void* out, int64_t ldo, const int32_t* starts, int n_seqs,
                            int total, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* lens, int max_len, int heads,
                            int causal, float scale, void* workspace, int64_t workspace_bytes);

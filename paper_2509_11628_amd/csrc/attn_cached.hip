@@ -11,9 +11,9 @@
 // dimension.  A page's bytes are asked for as soon as the registers of the page before are free: 16 KB per wave and 128 columns, 128 KB per
 // unit, always under way.
 //
-// What bounds it: memory.  One token of 8 sequences of 257 to 65 000 tokens, 32 heads over 8 of 128: 90 us for 437 MB, 4.9 TB/s (a large
-// copy moves 5.0); of one of 65 000 27 us and 8 for the join.  Short ones are a chain of waits: lists, table, bytes, the four waves' sums;
-// four sequences of 1 to 1200 tokens take 10 us.
+// What bounds it: memory.  One token of 8 sequences of 257 to 65 000 tokens, 32 heads over 8 of 128: 91 us for 437 MB, 4.8 TB/s (a large
+// copy moves 5.0); of one of 65 000 29 us and 5 for the join; of 1024 of about 1000 413 us for 2.2 GB.  Short ones are a chain of waits:
+// lists, table, bytes, the four waves' sums; four sequences of 1 to 1200 tokens take 13 us (14 between events).
 #include <algorithm>
 #include <cmath>
 
@@ -361,8 +361,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
   }
 }
 
-// Joins the splits of the rows of a tile of ROWS, four rows at a time, `quads` times per block: each wave sums every fourth split, in their
-// order, then the waves' sums are added.  Lane: four columns of rows lane / 32 and 2 + lane / 32.
+// Joins the splits of the rows of a tile of ROWS, four rows at a time, `quads` times per block: wave w sums the splits w, w + WAVES, ... in
+// their order, then the waves' sums are added.  Lane: four columns of rows lane / 32 and 2 + lane / 32.
 template <int HD, int ROWS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void attention_cached_join_kernel(const CachedArgs g, int quads) {
   constexpr int C = HD / 4;                        // lanes of a row
@@ -454,9 +454,9 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   p.tiles = rows / p.rows + n_seqs;
   p.resident = 2 * compute_units();
   // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (one
-  // token of a few sequences of up to 44 000: 24.9 us, 31.4 with 24), but no splits at all, and no second launch, up to 20 pages (four
-  // sequences of up to 1200: 14 us, 17.5 with splits of 8).  128 rows: 16 (931 + 238 + 16 + 17 tokens over 980, 314, 36 049 and 6026: 77
-  // us, 88 with 8, 85 with 24; the other way 256 tokens over 4096 and over 1024: 49 us, 39 with 8).
+  // token of 8 sequences of up to 43 654, 16 heads over 2: 20.6 us, 21.8 with 6 or 4, 30.5 with 24), but no splits at all, and no second
+  // launch, up to 20 pages (four sequences of up to 1200: 13.6 us, 17.4 with splits of 8).  128 rows: 16 (931 + 238 + 16 + 17 tokens over
+  // 980, 314, 36 049 and 6026: 77 us, 88 with 8, 85 with 24; the other way 256 tokens over 4096 and over 1024: 49 us, 39 with 8).
   p.least_pages = p.rows == 128 ? 16 : pages <= 20 ? 20 : 8;
   const int64_t whole = p.tiles * kv_heads;
   if (pages > p.least_pages) {
@@ -475,6 +475,8 @@ void launch_join(const CachedArgs& g, const Plan& p, hipStream_t st) {
   // a block per four rows while that leaves the chip room, else one per 32
   const int64_t quads = p.tiles * g.kv_heads * (ROWS / 4);
   const int each = quads > 8 * p.resident ? (ROWS / 4 < 8 ? ROWS / 4 : 8) : 1;
+  // Where few rows are joined, by 16 waves: a chain of waits, shorter the fewer splits a wave has (four tokens over 39 656, 28 heads over 4:
+  // 29.5 -> 25.0 us).  With more rows than the chip holds such blocks 4 are better (6 tokens over up to 12 234, 24 heads: 27.6 us, 31.3).
   const unsigned blocks = static_cast<unsigned>(quads / each);
   if (quads <= p.resident) attention_cached_join_kernel<HD, ROWS, 16><<<blocks, 1024, 0, st>>>(g, each);
   else attention_cached_join_kernel<HD, ROWS, 4><<<blocks, 256, 0, st>>>(g, each);
