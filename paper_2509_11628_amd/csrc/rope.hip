@@ -19,7 +19,6 @@ namespace {
 
 constexpr int kMaxHead = 128;
 
-
 struct RopeSide {
   const void* x;
   void* out;
@@ -256,7 +255,7 @@ Error launch_rope_axes(int dtype, const speca_rope& rope, const int32_t* positio
   if (!(eps >= 0.0f) || !std::isfinite(eps)) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: eps = %g", eps);
   SPECA_TRY(check_side("q", dtype, q, head_dim));
   if (k) SPECA_TRY(check_side("k", dtype, *k, head_dim));
-  if (!positions) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: positions is NULL");
+  if (!positions || reinterpret_cast<uintptr_t>(positions) % 4) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: positions is NULL or not aligned to int32");
   if (tokens == 0) return ok();
 
   RopeArgs g;

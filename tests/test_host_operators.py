@@ -132,3 +132,8 @@ def test_binding_refuses_what_does_not_fit(bd):
 
 def test_operator_struct_layouts(bd):
     assert C.sizeof(bd.Rope) == 4 * 15 and C.sizeof(bd.RopeIO) == 48 and C.sizeof(bd.KVCacheDesc) == 48 and C.sizeof(bd.KVTable) == 16
+
+
+def test_misaligned_lists_are_refused(bd):
+    assert _rope(bd, positions=A + 2) == bd.EINVAL
+    assert _packed(bd, starts=A + 2) == bd.EINVAL
