@@ -15,9 +15,14 @@ __device__ inline void widen(uint32_t b, float scale, uint32_t* out) {
   out[1] = *reinterpret_cast<const uint32_t*>(&hi);
 }
 // What the join needs to know of a sequence.
-struct Share {
+struct Share {                      // tiles of few rows
   int32_t splits, tiles;
   int64_t slot;                     // of its first unit; a sequence of one split has none
+};
+struct alignas(16) Stretch {        // tiles of 128 rows
+  int64_t from, per;                // position of its first tile, positions of a block
+  int32_t tiles, pages;
+  int32_t splits;                   // of every tile, one position each; 0: as the borders of the blocks have it
 };
 struct CachedArgs {
   const uint8_t *k, *v;
@@ -27,7 +32,7 @@ struct CachedArgs {
   int64_t ldq, ldo;
   Packed seqs;
   const int32_t *lens, *table;
-  Share* shares;                    // of every sequence, for the join
+  void* shares;                     // Share or Stretch of every sequence, for the join
   float *part, *stats;              // of splits, by slot: O [rows of a tile][HD], and maximum and sum [2][rows]
   int32_t table_ld, pages, kv_heads, group;
   int32_t max_len, resident, least_pages, slots;
@@ -35,7 +40,7 @@ struct CachedArgs {
   float scale_log2e;
 };
 
-// How the work is dealt.  The host knows no lengths, so every wave works it out from the lists on the device, 64 sequences at a time.  A
+// How the work of few rows is dealt.  The host knows no lengths, so every wave works it out from the lists on the device, 64 sequences at a time.  A
 // unit is one row tile of one key head over one split of its sequence's range of pages; ranges longer than split_pages are split evenly.
 // With `whole` units if nothing is split and W pages to visit in all, split_pages = W / E makes at most min(E + whole, 2 E) units of split
 // ranges.
@@ -131,6 +136,16 @@ struct Found {
   int each;                         // pages of a split
   int64_t slot;
 };
+// Unit of this block in a round of the grid, or -1.  Blocks b, b + 8, ... run on the same XCD: each XCD gets a run of the round's units,
+// which share keys, and as many as the others.  (With the XCDs filled one after the other, us: 256 tokens over 4096 and over 1024, 16 heads
+// of 72, 52 instead of 43; one token of 8 sequences of up to 43 654, 16 heads over 2, 20.6 instead of 17.9.)
+__device__ inline int64_t unit_of_block(int64_t round, int64_t units) {
+  const int64_t done = round * gridDim.x;
+  const int here = static_cast<int>(min(units - done, static_cast<int64_t>(gridDim.x))), b = blockIdx.x;
+  if (gridDim.x % 8) return b < here ? done + b : -1;
+  const int each = (here + 7) / 8, at = b % 8 * each + b / 8;
+  return b / 8 < each && at < here ? done + at : -1;
+}
 // Where a search has come to: the units of a block rise, so the next one begins there (one token of 1024 sequences of about 300: 267 -> 191 us).
 struct Place {
   int s0 = 0;
@@ -176,6 +191,21 @@ __device__ inline Found find_unit(const CachedArgs& g, const Deal& d, int64_t u,
 
 // Keys that new token `tok` of n sees, of `held` in the sequence of which the first `len` count.
 __device__ inline int keys_of(const CachedArgs& g, int held, int len, int n, int tok) { return g.causal ? max(0, min(len, held - n + tok + 1)) : len; }
+
+// How the work of tiles of 128 rows is dealt.  The tiles stand in line, sequence by sequence, head by head.
+//   Borders: a tile is as long as its pages and kTileCost positions more, and block k takes positions k per .. (k + 1) per - 1, so that all
+// blocks that fit on the chip end together.  A border less than kLeastPart pages from either end of a tile's pages moves to that end of the
+// tile.  What a block has of a tile that it shares with others goes to slot 2 k (it begins at the border of block k) or 2 k + 1.
+//   Units: a position is a tile, or one of its even splits of at least kLeastPages pages, and its number is its slot.  Taken where one round
+// of them ends sooner (few tiles: 256 tokens over 4096 and over 1024, 16 heads of 72: 43 us), and where no sequence is longer than
+// kLeastPages pages: then nothing is split, and a block takes every so many.
+// With whole rounds of even splits instead of borders (us): a frame of 1590 tokens over 27 286, 24 heads of 128, 648 instead of 618; a prompt of
+// 4096 tokens over itself, causal, 32 heads over 8, 286 instead of 174; 512 tokens over 8192 124 instead of 106.  A tile's cost of 6 or 9
+// positions instead of 4: 0.2 and 1.2 % slower over 37 batches.
+constexpr int kTileCost = 4, kLeastPart = 8, kLeastPages = 16;
+// Causal tiles see the more pages the later they are: the first, the last, the second, ... so that neighbours have the same work together.
+__device__ inline int tile_in_line(int j, int tiles, bool causal) { return !causal ? j : j & 1 ? tiles - 1 - (j >> 1) : j >> 1; }
+__device__ inline int place_in_line(int tile, int tiles, bool causal) { return !causal ? tile : tile < (tiles + 1) / 2 ? 2 * tile : 2 * (tiles - 1 - tile) + 1; }
 
 // 128 rows a tile, head_dim 64, 72 or 128 (attn_cached_tile.hip).
 void launch_attention_cached_tile(const CachedArgs& g, int head_dim, unsigned blocks, hipStream_t st);

@@ -47,15 +47,12 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
   const Deal d = deal<ROWS>(g);
   if (g.shares && blockIdx.x == 0 && wave == 0) {
     Place all;
-    find_unit<ROWS>(g, d, 0, g.shares, &all);
+    find_unit<ROWS>(g, d, 0, static_cast<Share*>(g.shares), &all);
   }
-  // Blocks b, b + 8, ... run on the same XCD: a round of the grid gives each XCD a run of units, which share keys where rows are many.
-  const int per_xcd = gridDim.x / 8;
   Place search;
-  for (int64_t round = 0;; ++round) {
-    const int64_t unit = gridDim.x % 8 ? round * gridDim.x + blockIdx.x : (round * 8 + blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-    if (round * gridDim.x >= d.units) break;
-    if (unit >= d.units) continue;
+  for (int64_t round = 0; round * gridDim.x < d.units; ++round) {
+    const int64_t unit = unit_of_block(round, d.units);
+    if (unit < 0) continue;
     const Found f = find_unit<ROWS>(g, d, unit, nullptr, &search);
     if (f.seq < 0 || (f.splits > 1 && f.slot + f.at >= g.slots)) continue;        // (offsets that overlap: there is no room for their sums)
     const int tile = f.at % f.tiles, split = f.at / f.tiles % f.splits, head = f.at / f.tiles / f.splits, seq = f.seq;
@@ -377,14 +374,41 @@ __global__ __launch_bounds__(64 * WAVES) void attention_cached_join_kernel(const
   packed_rows(g.seqs, seq, &start, &n);
   const int64_t r0 = static_cast<int64_t>(tile - packed_first_tile(g.seqs, seq, g.group, ROWS, 0)) * ROWS, rows = static_cast<int64_t>(n) * g.group;
   if (r0 < 0 || r0 + part * quads * 4 >= rows) return;
-  const Share f = g.shares[seq];
-  if (f.splits == 1 || f.slot + static_cast<int64_t>(f.tiles) * f.splits * g.kv_heads > g.slots) return;
-  const int64_t first = f.slot + static_cast<int64_t>(head) * f.splits * f.tiles + r0 / ROWS;
+  int splits;
+  int64_t first, next;                             // slot of the first split, and what lies between the second's and the others'
+  int64_t second;
+  if constexpr (ROWS == 128) {
+    const Stretch f = static_cast<const Stretch*>(g.shares)[seq];
+    const int64_t place = static_cast<int64_t>(head) * f.tiles + place_in_line(static_cast<int>(r0 / ROWS), f.tiles, g.causal);
+    if (f.splits) {
+      splits = f.splits;
+      first = f.from + place * splits;
+      second = first + 1;
+      next = 1;
+      if (splits == 1 || first + splits > g.slots) return;
+    } else {
+      const int64_t at = f.from + place * (f.pages + kTileCost);
+      const int64_t lo = (at + kLeastPart + f.per - 1) / f.per, hi = (at + f.pages - kLeastPart) / f.per;       // borders inside the tile
+      if (hi < lo || 2 * hi >= g.slots) return;
+      splits = static_cast<int>(hi - lo + 2);
+      first = 2 * lo - 1;
+      second = 2 * lo;
+      next = 2;
+    }
+  } else {
+    const Share f = static_cast<const Share*>(g.shares)[seq];
+    if (f.splits == 1 || f.slot + static_cast<int64_t>(f.tiles) * f.splits * g.kv_heads > g.slots) return;
+    splits = f.splits;
+    first = f.slot + static_cast<int64_t>(head) * f.splits * f.tiles + r0 / ROWS;
+    second = first + f.tiles;
+    next = f.tiles;
+  }
+  auto slot_of = [&](int s) { return s == 0 ? first : second + (s - 1) * next; };
   for (int quad = part * quads; quad < (part + 1) * quads && r0 + quad * 4 < rows; ++quad) {
-    auto stat = [&](int s, int which, int r) { return g.stats[((first + static_cast<int64_t>(s) * f.tiles) * 2 + which) * ROWS + quad * 4 + r]; };
+    auto stat = [&](int s, int which, int r) { return g.stats[(slot_of(s) * 2 + which) * ROWS + quad * 4 + r]; };
 
     float top = -INFINITY;                           // of row lane % 4, over the splits of this lane, then of all
-    for (int s = tid >> 2; s < f.splits; s += 16 * WAVES) top = fmaxf(top, stat(s, 0, tid & 3));
+    for (int s = tid >> 2; s < splits; s += 16 * WAVES) top = fmaxf(top, stat(s, 0, tid & 3));
     for (int off = 4; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
     if (lane < 4) tops[wave][lane] = top;
     __syncthreads();
@@ -400,12 +424,12 @@ __global__ __launch_bounds__(64 * WAVES) void attention_cached_join_kernel(const
       off[half] = m[half] == -INFINITY ? 0.0f : m[half] * g.scale_log2e;
     }
 #pragma unroll 8
-    for (int s = wave; s < f.splits; s += WAVES)
+    for (int s = wave; s < splits; s += WAVES)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int r = 2 * half + (lane >> 5);
         const float ms = stat(s, 0, r), l = stat(s, 1, r);
-        const floatx4 x = *reinterpret_cast<const floatx4*>(g.part + ((first + static_cast<int64_t>(s) * f.tiles) * ROWS + quad * 4 + r) * HD + 4 * (col < C ? col : 0));
+        const floatx4 x = *reinterpret_cast<const floatx4*>(g.part + (slot_of(s) * ROWS + quad * 4 + r) * HD + 4 * (col < C ? col : 0));
         // a split without a finite score has weight 0, unless all are so: then NaN where keys were seen, 0 elsewhere
         const float w = ms == -INFINITY ? (m[half] == -INFINITY ? 1.0f : 0.0f) : fast_exp2(ms * g.scale_log2e - off[half]);
         total[half] += ms == -INFINITY && w == 0.0f ? 0.0f : l * w;
@@ -455,15 +479,15 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   p.resident = 2 * compute_units();
   // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (one
   // token of 8 sequences of up to 43 654, 16 heads over 2: 20.6 us, 21.8 with 6 or 4, 30.5 with 24), but no splits at all, and no second
-  // launch, up to 20 pages (four sequences of up to 1200: 13.6 us, 17.4 with splits of 8).  128 rows: 16 (931 + 238 + 16 + 17 tokens over
-  // 980, 314, 36 049 and 6026: 77 us, 88 with 8, 85 with 24; the other way 256 tokens over 4096 and over 1024: 49 us, 39 with 8).
-  p.least_pages = p.rows == 128 ? 16 : pages <= 20 ? 20 : 8;
+  // launch, up to 20 pages (four sequences of up to 1200: 13.6 us, 17.4 with splits of 8).
+  p.least_pages = p.rows == 128 ? kLeastPages : pages <= 20 ? 20 : 8;
   const int64_t whole = p.tiles * kv_heads;
   if (pages > p.least_pages) {
-    p.slots = std::min<int64_t>(4 * p.resident, whole * ((pages + p.least_pages - 1) / p.least_pages));
+    p.slots = p.rows == 128 ? 2 * std::min<int64_t>(p.resident, (whole * (pages + kTileCost) + kLeastPages - 1) / kLeastPages)
+                            : std::min<int64_t>(4 * p.resident, whole * ((pages + p.least_pages - 1) / p.least_pages));
     p.part_bytes = p.slots * p.rows * head_dim * static_cast<int64_t>(sizeof(float));
     p.stat_bytes = p.slots * 2 * p.rows * static_cast<int64_t>(sizeof(float));
-    p.bytes = p.part_bytes + p.stat_bytes + n_seqs * static_cast<int64_t>(sizeof(Share));
+    p.bytes = p.part_bytes + p.stat_bytes + n_seqs * static_cast<int64_t>(std::max(sizeof(Share), sizeof(Stretch)));
   }
   p.units = whole + p.slots;
   return p;
@@ -538,7 +562,7 @@ Error launch_attention_cached(int dtype, const speca_kv_cache& c, const speca_kv
   g.lens = a.lens; g.table = t.page;
   g.part = static_cast<float*>(workspace);
   g.stats = p.bytes ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes) : nullptr;
-  g.shares = p.bytes ? reinterpret_cast<Share*>(static_cast<char*>(workspace) + p.part_bytes + p.stat_bytes) : nullptr;
+  g.shares = p.bytes ? static_cast<char*>(workspace) + p.part_bytes + p.stat_bytes : nullptr;
   g.table_ld = t.ld; g.pages = c.pages; g.kv_heads = c.kv_heads; g.group = a.heads / c.kv_heads;
   g.max_len = static_cast<int>(std::min<int64_t>(a.max_len, static_cast<int64_t>(t.ld) * PAGE));
   g.resident = p.resident; g.least_pages = p.least_pages; g.slots = static_cast<int32_t>(p.slots);
