@@ -11,9 +11,9 @@
 // dimension.  A page's bytes are asked for as soon as the registers of the page before are free: 16 KB per wave and 128 columns, 128 KB per
 // unit, always under way.
 //
-// What bounds it: memory.  One token of 8 sequences of 257 to 65 000 tokens, 32 heads over 8 of 128: 91 us for 437 MB, 4.8 TB/s (a large
-// copy moves 5.0); of one of 65 000 29 us and 5 for the join; of 1024 of about 1000 413 us for 2.2 GB.  Short ones are a chain of waits:
-// lists, table, bytes, the four waves' sums; four sequences of 1 to 1200 tokens take 13 us (14 between events).
+// What bounds it: memory.  One token of 8 sequences of 257 to 65 000 tokens, 32 heads over 8 of 128: 90 us for 437 MB, 4.9 TB/s (a large
+// copy moves 5.0); of 1024 of about 1000 413 us for 2.2 GB.  Short ones are a chain of waits: lists, table, bytes, the four waves' sums;
+// four sequences of 1 to 1200 tokens take 13 us.
 #include <algorithm>
 #include <cmath>
 
@@ -477,9 +477,9 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   p.rows = mean <= 16 ? 16 : mean <= 32 || head_dim < 64 ? 32 : 128;
   p.tiles = rows / p.rows + n_seqs;
   p.resident = 2 * compute_units();
-  // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (one
-  // token of 8 sequences of up to 43 654, 16 heads over 2: 20.6 us, 21.8 with 6 or 4, 30.5 with 24), but no splits at all, and no second
-  // launch, up to 20 pages (four sequences of up to 1200: 13.6 us, 17.4 with splits of 8).
+  // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (33 tokens
+  // of 13 sequences of up to 9756, 28 heads over 4: 20.9 us, 22.1 with 6, 23.9 with 4, 27.5 with 24), but no splits at all, and no second
+  // launch, up to 20 pages (four sequences of up to 1200: 13.8 us, 18.2 with splits of 6).
   p.least_pages = p.rows == 128 ? kLeastPages : pages <= 20 ? 20 : 8;
   const int64_t whole = p.tiles * kv_heads;
   if (pages > p.least_pages) {

@@ -11,9 +11,9 @@
 // go to place [half][tile of 16 dimensions][lane], so a fragment is one read of 16 bytes per lane, all lanes in a row.
 //
 // What bounds it: the vector unit (exponentials, maxima, widening) and the LDS reads beside the matrix instructions, at two blocks per
-// unit.  A frame of 1590 tokens over 27 286, 24 heads of 128: 645 us, 826 TFLOP/s, 27 of it the join.  On the way there, us: widening in
-// every wave's registers instead (rows of 64 a wave) 1150; through LDS 950; without bank conflicts of the writes 745 with those of the
-// values, 683 with those of the keys gone; without registers that spill to memory, whose restores wait for the bytes on their way, 647
+// unit.  A frame of 1590 tokens over 27 286, 24 heads of 128: 615 to 630 us with the join, 845 to 865 TFLOP/s.  On the way there, us:
+// widening in every wave's registers instead (rows of 64 a wave) 1150; through LDS 950; without bank conflicts of the writes 745 with those
+// of the values, 683 with those of the keys gone; without registers that spill to memory, whose restores wait for the bytes on their way, 647
 // (three or four fragments ahead instead of two spill again: 650 and 715; keys in units of 8 bytes, which spares the turn below, 802).
 #include <type_traits>
 
