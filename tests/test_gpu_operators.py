@@ -507,6 +507,40 @@ def test_cached_many_sequences(hd, H, tokens):
     _cached_check(bd, new, lens, H, 2, hd, True, seed=5)
 
 
+@pytest.mark.parametrize("hd", [64, 72, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_cached_more_tiles_than_fit(hd, causal):
+    """More tiles than the chip holds blocks, so that blocks end inside tiles: few long sequences, and many of which some are short, empty or
+    without new tokens."""
+    bd = _bd()
+    _cached_check(bd, [2300, 30], [2400, 2000], 16, 16, hd, causal, seed=6)
+    rng = np.random.default_rng(1)
+    lens = [int(n) for n in rng.integers(0, 1500, 100)]
+    lens[3], lens[99], lens[50] = 0, 1500, 40
+    new = [0 if s % 13 == 5 else int(rng.integers(1, 80)) for s in range(100)]
+    _cached_check(bd, new, lens, 24, 6, hd, causal, seed=7)
+
+
+@pytest.mark.parametrize("hd", [64, 72, 128])
+def test_cached_nan_where_blocks_end_inside_tiles(hd):
+    """A NaN among the values reaches every row of its head that sees it, in whichever part of a tile it lies, and no other feature."""
+    bd = _bd()
+    H, n, new = 16, 2500, 2300
+    cache, table, _ = _fill(bd, [n], H, hd)
+    q = ref.randn((new, H, hd), torch.bfloat16, 9)
+    run = lambda: bd.attention_cached(q, ref.starts_of([new]), cache, _dev(table), _dev([n]), causal=True)  # noqa: E731
+    clean = run()
+    for at in (3, 700, 1400, n - 1):
+        page, place = int(table[0, at // 64]), ref.PLACE[at % 64]
+        old = cache.v.clone()
+        cache.v[page, 5, 7, place] = 0x7F
+        got = run()
+        cache.v.copy_(old)
+        see = max(0, at - (n - new))                     # the first new token that sees it
+        assert torch.equal(got[:see], clean[:see]) and torch.equal(got[:, :5], clean[:, :5]) and torch.equal(got[:, 6:], clean[:, 6:])
+        assert bool(got[see:, 5, 7].isnan().all()) and torch.equal(got[:, 5, 8:], clean[:, 5, 8:]) and torch.equal(got[:, 5, :7], clean[:, 5, :7])
+
+
 @pytest.mark.parametrize("hd", [64, 128])
 def test_cached_one_and_many_tokens_in_one_call(hd):
     """Single tokens beside a whole prompt, and empty sequences alone."""
