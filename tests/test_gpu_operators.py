@@ -507,6 +507,26 @@ def test_cached_many_sequences(hd, H, tokens):
     _cached_check(bd, new, lens, H, 2, hd, True, seed=5)
 
 
+@pytest.mark.parametrize("pad,offset", [(8, 8), (4, 4), (1, 0), (3, 5)])
+@pytest.mark.parametrize("hd", [16, 32, 64, 72, 128])
+def test_cached_many_rows_strides(pad, offset, hd):
+    """Many rows per sequence with queries and outputs at any alignment and distance: the bits of contiguous ones."""
+    bd = _bd()
+    cache, table, _ = _fill(bd, [2000, 90], 2, hd)
+    q = ref.randn((130, 8, hd), torch.bfloat16, 4)
+    cu, held = ref.starts_of([50, 80]), _dev([2000, 90])
+    plain = bd.attention_cached(q, cu, cache, _dev(table), held)
+    strided = bd.attention_cached(ref.strided(q, pad, offset), cu, cache, _dev(table), held, out=ref.strided(torch.zeros_like(q), pad, offset))
+    assert torch.equal(plain, strided)
+
+
+@pytest.mark.parametrize("hd", [16, 32])
+@pytest.mark.parametrize("causal", [False, True])
+def test_cached_many_rows_of_small_heads(hd, causal):
+    bd = _bd()
+    _cached_check(bd, [70, 300, 1], [3000, 310, 64], 6, 2, hd, causal, seed=8)
+
+
 @pytest.mark.parametrize("hd", [64, 72, 128])
 @pytest.mark.parametrize("causal", [False, True])
 def test_cached_more_tiles_than_fit(hd, causal):
