@@ -124,6 +124,14 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const RopeArgs g) {
     for (int j = 0; j < VP; ++j) angle(u * VP + j, &cs[j], &sn[j]);
   }
 
+  // Only pairs that turn: by an angle of 0 a feature would not stay as it is, since 0 x its neighbour is NaN where that is infinite or NaN.
+  // (Selected: as branches 146 us instead of 141.)
+  auto turn = [](bool turns, float& a, float& b, float c, float s) {
+    const float x = fmaf(a, c, -(b * s)), y = fmaf(a, s, b * c);
+    a = turns ? x : a;
+    b = turns ? y : b;
+  };
+
   int first = chunk * g.steps_per_wave, last = first + g.steps_per_wave;       // steps of this wave, counted from the side's first
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -184,19 +192,12 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(const RopeArgs g) {
         float(&q)[VP] = b[i];
         if constexpr (HALVES || VP == 1) {
 #pragma unroll
-          for (int j = 0; j < VP; ++j) {
-            const float c = fmaf(p[j], cs[j], -(q[j] * sn[j]));
-            q[j] = fmaf(p[j], sn[j], q[j] * cs[j]);
-            p[j] = c;
-          }
+          for (int j = 0; j < VP; ++j) turn(u * VP < pairs, p[j], q[j], cs[j], sn[j]);
         } else {
 #pragma unroll
-          for (int j = 0; j < VP; j += 2) {
-            const float c = fmaf(p[j], cs[j / 2], -(p[j + 1] * sn[j / 2])), d = fmaf(q[j], cs[VP / 2 + j / 2], -(q[j + 1] * sn[VP / 2 + j / 2]));
-            p[j + 1] = fmaf(p[j], sn[j / 2], p[j + 1] * cs[j / 2]);
-            q[j + 1] = fmaf(q[j], sn[VP / 2 + j / 2], q[j + 1] * cs[VP / 2 + j / 2]);
-            p[j] = c;
-            q[j] = d;
+          for (int j = 0; j < VP; ++j) {
+            float(&x)[VP] = j < VP / 2 ? p : q;
+            turn(u * VP + j < pairs, x[2 * j % VP], x[2 * j % VP + 1], cs[j], sn[j]);
           }
         }
         if (live && step * per + sub < heads) rope_store<VP, HALVES>(out + step * per * g.hd, lo, hi, p, q);

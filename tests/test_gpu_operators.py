@@ -812,3 +812,33 @@ def test_captured_step_replayed_over_growing_sequences():
             assert torch.equal(a, b), turn
         for t in (past, held, pos):
             t += 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("normed", [False, True])
+def test_rope_features_that_stay(dtype, halves, normed):
+    """Features behind those that turn are neither turned nor mixed: infinities, NaN and -0 among them stay where they are."""
+    bd = _bd()
+    dt, tokens, H = _dt(dtype), 9, 5
+    # four pairs a lane, rotations that end inside a lane, one pair a lane (heads of 30, views off their alignment)
+    for hd, dims, pad, offset in ((72, (32, 32), 0, 0), (128, (64,), 0, 0), (64, (10, 6), 0, 0), (72, (12, 2), 0, 0), (30, (6, 10), 0, 0), (72, (32, 32), 1, 1)):
+        R, g = sum(dims), torch.Generator(device="cuda").manual_seed(hd)
+        x = ref.randn((tokens, H, hd), dt, hd + R)
+        for i, bad in enumerate((math.inf, -math.inf, math.nan, -0.0, -0.0)):
+            x[i, i % H, R + 2 * i % (hd - R)] = bad                 # even and odd ones: either side of what would be a pair
+            x[i + 2, (i + 1) % H, R + (2 * i + 1) % (hd - R)] = bad
+        x[8, :, R:] = -0.0
+        pos = torch.randint(0, 1000, (tokens, len(dims)), generator=g, device="cuda", dtype=torch.int32)
+        norm = 1.0 + ref.randn((hd,), dt, 3, 0.1) if normed else None
+        rope = bd.make_rope(dims, pairing=bd.ROPE_HALVES if halves else bd.ROPE_ADJACENT)
+        if pad or offset:
+            x = ref.strided(x, pad, offset)
+        for got in (bd.rope_axes(rope, pos, x, q_norm=norm), bd.rope_axes(rope, pos, x.clone(), x, norm, norm)[1]):
+            want, tol = ref.rope(x, pos, dims, [10000.0] * 2, [1.0] * 2, halves, False, norm, 1e-6)
+            number = want.isfinite()
+            assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.isinf(), want.isinf()), (hd, dims)
+            assert bool((((got.double() - want).abs() <= tol) | ~number).all()), (hd, dims)
+            assert torch.equal(got[..., R:].signbit() & number[..., R:], want[..., R:].signbit() & number[..., R:]), (hd, dims)
+            if not normed:
+                assert bool(((got[..., R:] == x[..., R:]) | x[..., R:].isnan()).all()), (hd, dims)
