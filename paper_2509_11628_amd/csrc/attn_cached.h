@@ -2,6 +2,7 @@
 #pragma once
 
 #include "attn_lane.h"
+#include "deal.h"
 #include "operators.h"
 
 namespace speca {
@@ -41,13 +42,8 @@ struct CachedArgs {
 };
 
 // How the work of few rows is dealt.  The host knows no lengths, so every wave works it out from the lists on the device, 64 sequences at a time.  A
-// unit is one row tile of one key head over one split of its sequence's range of pages; ranges longer than split_pages are split evenly.
-// With `whole` units if nothing is split and W pages to visit in all, split_pages = W / E makes at most min(E + whole, 2 E) units of split
-// ranges.
-//   whole <= resident / 4:  E = resident - whole: one round of the blocks that fit on the chip
-//   otherwise:              E = R resident - whole for the R of 1 to 4 whose rounds x (longest unit + 4 pages that it takes to begin and end one) are
-//                           fewest (E = 2 resident where no R has room)
-// and never more than 4 resident of them, which is what the workspace has room for.
+// unit is one row tile of one key head over one split of its sequence's range of pages; ranges longer than split_pages, which deal.h chooses, are
+// split evenly.
 struct Deal {
   int tiles, pages;                 // of the lane's sequence in the first 64
   int64_t units;                    // of all
@@ -72,7 +68,6 @@ __device__ inline int64_t sum_of_wave(int64_t x, int lanes) {
   for (int off = 1; off < lanes && off < 64; off <<= 1) x += __shfl_xor(x, off, 64);
   return of_lane(x, 0);
 }
-__device__ inline int splits_of(int pages, int split_pages) { return pages > split_pages ? (pages + split_pages - 1) / split_pages : 1; }
 __device__ inline int max_of_wave(int x, int lanes) {
   for (int off = 1; off < lanes && off < 64; off <<= 1) x = max(x, __shfl_xor(x, off, 64));
   return __builtin_amdgcn_readlane(x, 0);
@@ -92,8 +87,6 @@ __device__ inline Deal deal(const CachedArgs& g) {
   }
   work = sum_of_wave(work, g.seqs.n) * g.kv_heads;
   whole = sum_of_wave(whole, g.seqs.n) * g.kv_heads;
-  auto pages_for = [&](int64_t ranges) { return static_cast<int>(max(static_cast<int64_t>(g.least_pages), (work + ranges - 1) / ranges)); };
-  // units of all sequences, and pages of the longest
   auto count = [&](int split_pages, int64_t* units, int* longest) {
     int splits = splits_of(d.pages, split_pages), most = d.tiles ? (d.pages + splits - 1) / splits : 0;
     int64_t sum = static_cast<int64_t>(d.tiles) * splits;
@@ -107,26 +100,9 @@ __device__ inline Deal deal(const CachedArgs& g) {
     *units = sum_of_wave(sum, g.seqs.n) * g.kv_heads;
     if (longest) *longest = max_of_wave(most, g.seqs.n);
   };
-  const int64_t resident = g.resident;
-  if (4 * whole <= resident) {
-    d.split_pages = pages_for(resident - whole);
-    count(d.split_pages, &d.units, nullptr);
-    return d;
-  }
-  int64_t best = -1;
-  for (int rounds = 1; rounds <= 4 || best < 0; ++rounds) {
-    const int64_t ranges = rounds <= 4 ? rounds * resident - whole : 2 * resident;
-    if (ranges <= 0) continue;
-    const int split_pages = pages_for(ranges);
-    int64_t units;
-    int longest;
-    count(split_pages, &units, &longest);
-    const int64_t cost = (units + resident - 1) / resident * (longest + 4);
-    if (best >= 0 && cost >= best) continue;
-    best = cost;
-    d.split_pages = split_pages;
-    d.units = units;
-  }
+  const Cut cut = cut_few_rows(work, whole, g.resident, g.least_pages, (g.max_len + PAGE - 1) / PAGE, count);
+  d.split_pages = cut.split_pages;
+  d.units = cut.units;
   return d;
 }
 // Sequence of unit u, u's number within it and the slot of its first unit.  (u rises through tiles first, then splits, then heads: blocks

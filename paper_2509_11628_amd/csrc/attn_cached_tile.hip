@@ -101,7 +101,7 @@ __device__ inline Line lay_out(const CachedArgs& g, const Lists& lists) {
     most = max_of_wave(most, g.seqs.n);
     // (a block between borders has parts of two tiles as a rule)
     if (units <= g.resident && most <= per + kTileCost) return {units, 1, split_pages};
-    split_pages = static_cast<int>(max(static_cast<int64_t>(kLeastPages), rounded_up(work, room)));
+    split_pages = pages_of_split(rounded_up(work, room), kLeastPages, longest);
   }
   return {weight, per, 0};
 }

@@ -1,5 +1,8 @@
 """Refusals of the operators around attention, all of them decided on the host ahead of any GPU work, and their workspace sizes."""
 import ctypes as C
+import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -137,3 +140,15 @@ def test_operator_struct_layouts(bd):
 def test_misaligned_lists_are_refused(bd):
     assert _rope(bd, positions=A + 2) == bd.EINVAL
     assert _packed(bd, starts=A + 2) == bd.EINVAL
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="no host C++ compiler")
+def test_how_few_rows_are_cut(tmp_path):
+    """csrc/deal.h on the host: no more units than the workspace has room for, sums beyond 32 bits."""
+    exe = str(tmp_path / "deal")
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-static-libubsan", os.path.join(here, "deal_driver.cpp"), "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and "dealing is right" in r.stdout, r.stdout + r.stderr
