@@ -15,9 +15,11 @@ constexpr int pages_of_split(int64_t even, int least, int most) { return even <=
 // Few rows: `whole` units if nothing is cut, `work` pages to visit in all.  Splits of work / E pages make at most min(E + whole, 2 E) units of ranges
 // that are cut, and
 //   whole <= resident / 4:  E = resident - whole: one round of the blocks that fit on the chip
-//   otherwise:              E = R resident - whole for the R of 1 to 4 whose rounds x (longest unit + 4 pages that it takes to begin and end one) are
-//                           fewest (E = 2 resident where no R has room)
-// which is never more than 4 resident units: what the workspace has room for.
+//   otherwise:              the E of R resident - whole, R = 1 to 4, and of 2 resident where that is more than the last of them, whose rounds x
+//                           (longest unit + 4 pages that it takes to begin and end one) are fewest
+// which is never more than 4 resident units: what the workspace has room for.  (Close to whole = 4 resident the first four leave room for next to
+// no range, and a long sequence among short ones whole.  One token of 255 sequences, 8 heads of 128, 254 of 512 tokens and one of 65 536: 413 us
+// with the four alone, 99 with the last; of 224 121 and 94; of 200 of up to 1000, where nothing is gained, 47 and 49.)
 // count(split_pages, &units, &longest): units of all sequences, and pages of the longest of them (not asked for: nullptr).
 struct Cut {
   int split_pages;
@@ -33,9 +35,9 @@ constexpr Cut cut_few_rows(int64_t work, int64_t whole, int64_t resident, int le
     return best;
   }
   int64_t lowest = -1;
-  for (int rounds = 1; rounds <= 4 || lowest < 0; ++rounds) {
+  for (int rounds = 1; rounds <= 5; ++rounds) {
     const int64_t ranges = rounds <= 4 ? rounds * resident - whole : 2 * resident;
-    if (ranges <= 0) continue;
+    if (ranges <= 0 || (rounds == 5 && 4 * resident - whole >= ranges)) continue;
     Cut cut{pages_of_split((work + ranges - 1) / ranges, least, most), 0};
     int longest = 0;
     count(cut.split_pages, &cut.units, &longest);

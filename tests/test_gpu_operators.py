@@ -842,3 +842,12 @@ def test_rope_features_that_stay(dtype, halves, normed):
             assert torch.equal(got[..., R:].signbit() & number[..., R:], want[..., R:].signbit() & number[..., R:]), (hd, dims)
             if not normed:
                 assert bool(((got[..., R:] == x[..., R:]) | x[..., R:].isnan()).all()), (hd, dims)
+
+
+@pytest.mark.parametrize("n", [250, 255, 256])
+def test_cached_one_long_among_many_short(n):
+    """About as many single tokens as four rounds of blocks take, one of them over a long sequence."""
+    bd = _bd()
+    lens = [500 - s % 3 for s in range(n)]
+    lens[n // 2] = 512 * 64 - 5
+    _cached_check(bd, [1] * n, lens, 8, 8, 64, True, seed=4)

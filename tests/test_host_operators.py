@@ -144,7 +144,7 @@ def test_misaligned_lists_are_refused(bd):
 
 @pytest.mark.skipif(shutil.which("g++") is None, reason="no host C++ compiler")
 def test_how_few_rows_are_cut(tmp_path):
-    """csrc/deal.h on the host: no more units than the workspace has room for, sums beyond 32 bits."""
+    """csrc/deal.h on the host: no cliff in the number of sequences, no more units than the workspace has room for, sums beyond 32 bits."""
     exe = str(tmp_path / "deal")
     here = os.path.dirname(os.path.abspath(__file__))
     r = subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-static-libubsan", os.path.join(here, "deal_driver.cpp"), "-o", exe],
