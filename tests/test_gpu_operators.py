@@ -851,3 +851,56 @@ def test_cached_one_long_among_many_short(n):
     lens = [500 - s % 3 for s in range(n)]
     lens[n // 2] = 512 * 64 - 5
     _cached_check(bd, [1] * n, lens, 8, 8, 64, True, seed=4)
+
+
+@pytest.mark.parametrize("hd", [64, 72, 128])
+@pytest.mark.parametrize("new,lens,max_len", [([3, 5], [200, 150], 148), ([14, 9], [300, 150], 146), ([70, 90], [300, 260], 200), ([40], [4000], 3990), ([4, 1], [4000, 2000], 1997)])
+def test_cached_causal_bound_below_the_lengths(hd, new, lens, max_len):
+    """max_len cuts sequences off inside the new tokens, and well before them; what a new token sees follows from its place in the whole
+    sequence all the same.  Tiles of 16, 32 and 128 rows, split and not."""
+    bd = _bd()
+    H, Hkv = 4, 2
+    cache, table, twin = _fill(bd, lens, Hkv, hd, 11)
+    q = ref.randn((sum(new), H, hd), torch.bfloat16, 12)
+    got, at = bd.attention_cached(q, ref.starts_of(new), cache, _dev(table), _dev(lens), causal=True, max_len=max_len), 0
+    for s, (a, n) in enumerate(zip(new, lens)):
+        (k, held), (v, _) = twin.values(0, table[s], n), twin.values(1, table[s], n)
+        key = torch.arange(n, device="cuda")[None]
+        sees = held[None] & (key < max_len) & (key <= n - a + torch.arange(a, device="cuda")[:, None])
+        ref.close(got[at:at + a], *ref.attention(q[at:at + a], k, v, sees, 1.0 / math.sqrt(hd), BF16_P, torch.bfloat16), (s, a, n))
+        at += a
+
+
+@pytest.mark.parametrize("total", [3, 45, 200])
+def test_captured_attention_over_lists_that_change(total):
+    """One graph of attention over a table wide enough to be split, for every height of tiles: between its replays the lists on the device
+    change how the work is dealt (nothing split, one sequence split, all of them), and so do the tokens' sequences.  Each time the bits of an eager call."""
+    bd = _bd()
+    H, Hkv, hd, width, n = 8, 2, 128, 160, 3
+    table = _dev(_tables(3 * width, [width] * n, width))
+    cache = bd.KVCache.empty(3 * width, Hkv, hd)
+    rows = width * 64
+    for s in range(n):
+        k, v = ref.randn((rows, Hkv, hd), torch.bfloat16, 2 * s), ref.randn((rows, Hkv, hd), torch.bfloat16, 2 * s + 1)
+        bd.kv_store(cache, table[s:s + 1], _dev([0]), k, v, ref.starts_of([rows]))
+    q = ref.randn((total, H, hd), torch.bfloat16, 9)
+    third = total // 3
+    turns = [([0, third, 2 * third, total], [62, 0, 1150]), ([0, third, 2 * third, total], [70, 9001, 1151]), ([0, third, 2 * third, total], [rows, rows - 1, rows - 63]),
+             ([0, 0, 1, total], [rows, 5000, 300]), ([0, total, total, total], [rows, 17, 0]), ([0, third, 2 * third, total], [63, 1, 1151])]
+    starts, held = _dev(turns[0][0]), _dev(turns[0][1])
+    bd.attention_cached(q, starts, cache, table, held)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = bd.attention_cached(q, starts, cache, table, held)
+    for turn, (a, b) in enumerate(turns):
+        starts.copy_(_dev(a))
+        held.copy_(_dev(b))
+        want = bd.attention_cached(q, starts, cache, table, held)
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and not bool(out.isnan().any()), turn
+        for s in range(n):
+            if a[s + 1] > a[s] and b[s] == 0:
+                assert bool((out[a[s]:a[s + 1]] == 0).all())
