@@ -262,8 +262,9 @@ int speca_attention(void* hip_stream, int dtype, const void* qkv, void* out, int
  * (starts: DEVICE int32 [n_seqs + 1], rising; a sequence may be empty).  Tokens below starts[0] and from starts[n_seqs] on are
  * neither read nor written.  Offsets are clamped to 0 .. total, so none reads or writes outside the buffers. Everything is
  * asynchronous on hip_stream, whose device must be the current one; nothing is allocated, kept or synchronised, so calls may be
- * captured into a HIP graph.  No tokens (total = 0) is no work.  Errors: message via speca_last_error(NULL).  Results do not
- * depend on timing: the same inputs give the same bits. */
+ * captured into a HIP graph.  No tokens (total = 0) is no work; more tokens and heads than one launch can hold (from 2^26 tokens on in
+ * speca_rope_axes) are SPECA_EINVAL.  Errors: message via speca_last_error(NULL).  Results do not depend on timing: the same inputs give
+ * the same bits. */
 
 enum { SPECA_ROPE_ADJACENT = 0, SPECA_ROPE_HALVES = 1 };
 enum { SPECA_ROPE_PER_AXIS = 0, SPECA_ROPE_JOINT = 1 };

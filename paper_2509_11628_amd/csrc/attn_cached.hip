@@ -493,12 +493,15 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   return p;
 }
 
+// Rows to join, four by four, and how many fours a block takes: one while that leaves the chip room, else 32 rows.
+int64_t join_quads(const Plan& p, int kv_heads) { return p.tiles * kv_heads * (p.rows / 4); }
+int join_each(const Plan& p, int kv_heads) { return join_quads(p, kv_heads) > 8 * p.resident ? std::min(p.rows / 4, 8) : 1; }
+
 template <int HD, int ROWS>
 void launch_join(const CachedArgs& g, const Plan& p, hipStream_t st) {
   if (!p.slots) return;
-  // a block per four rows while that leaves the chip room, else one per 32
-  const int64_t quads = p.tiles * g.kv_heads * (ROWS / 4);
-  const int each = quads > 8 * p.resident ? (ROWS / 4 < 8 ? ROWS / 4 : 8) : 1;
+  const int64_t quads = join_quads(p, g.kv_heads);
+  const int each = join_each(p, g.kv_heads);
   // Where few rows are joined, by 16 waves: a chain of waits, shorter the fewer splits a wave has (four tokens over 39 656, 28 heads over 4:
   // 29.5 -> 25.0 us).  With more rows than the chip holds such blocks 4 are better (6 tokens over up to 12 234, 24 heads: 27.6 us, 31.3).
   const unsigned blocks = static_cast<unsigned>(quads / each);
@@ -550,7 +553,8 @@ Error launch_attention_cached(int dtype, const speca_kv_cache& c, const speca_kv
   if (!(a.scale >= 0.0f) || !std::isfinite(a.scale)) SPECA_FAIL(SPECA_EINVAL, "%s: scale = %g", who, a.scale);
   if (a.seqs.total == 0) return ok();
   const Plan p = plan_of(a.seqs.n, a.seqs.total, a.max_len, a.heads, c.kv_heads, c.head_dim);
-  if (p.tiles * c.kv_heads * (p.rows / 4) > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "%s: %d tokens of %d heads are too many for one call", who, a.seqs.total, a.heads);
+  if (join_quads(p, c.kv_heads) > 0x7FFFFFFF || (p.slots && join_quads(p, c.kv_heads) / join_each(p, c.kv_heads) > kMaxBlocks))
+    SPECA_FAIL(SPECA_EINVAL, "%s: %d tokens of %d heads are too many for one call", who, a.seqs.total, a.heads);
   if (p.bytes && (!workspace || workspace_bytes < p.bytes || reinterpret_cast<uintptr_t>(workspace) % 16))
     SPECA_FAIL(SPECA_EINVAL, "%s: a workspace of %lld bytes, 16-byte aligned, is needed (given: %lld)", who, static_cast<long long>(p.bytes), static_cast<long long>(workspace ? workspace_bytes : 0));
   CachedArgs g;

@@ -841,7 +841,7 @@ Error launch_hd(const void* qkv, void* out, int64_t ldo, int rows, int T, int H,
 template <int HD>
 Error launch_packed_hd(const PackedAttention& a, hipStream_t st) {
   const int64_t tiles = packed_tiles(a.seqs, 1, 128, 0), blocks = tiles * a.heads;
-  if (blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "speca_attention_packed: %d tokens of %d heads are too many for one call", a.seqs.total, a.heads);
+  if (blocks > kMaxBlocks) SPECA_FAIL(SPECA_EINVAL, "speca_attention_packed: %d tokens of %d heads are too many for one call", a.seqs.total, a.heads);
   const TileArgs g = {static_cast<const uint16_t*>(a.q), static_cast<const uint16_t*>(a.k), static_cast<const uint16_t*>(a.v), static_cast<uint16_t*>(a.out),
                       a.ldq, a.ldk, a.ldv, a.ldo, 0, a.heads, a.heads / a.kv_heads, a.seqs, static_cast<int32_t>(tiles), 1.4426950408889634f * a.scale};
   if (a.causal) attention_dma_kernel<HD, CAUSAL><<<static_cast<unsigned>(blocks), 256, 0, st>>>(g);

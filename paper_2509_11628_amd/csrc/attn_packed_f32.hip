@@ -279,7 +279,7 @@ Error launch_hd(const Args& g, hipStream_t st) {
   // 32 queries per block read every key and value half as often; 16 keep the chip busy when there are few of them (above: 396 blocks of 32)
   const bool two = static_cast<int64_t>(a.seqs.total / 32) * a.heads >= 512;
   const int64_t blocks = packed_tiles(a.seqs, 1, two ? 32 : 16, 0) * a.heads;
-  if (blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "speca_attention_packed: %d tokens of %d heads are too many for one call", a.seqs.total, a.heads);
+  if (blocks > kMaxBlocks) SPECA_FAIL(SPECA_EINVAL, "speca_attention_packed: %d tokens of %d heads are too many for one call", a.seqs.total, a.heads);
   if (two) launch_qt<T, HD, 2>(g, wide, static_cast<unsigned>(blocks), st);
   else launch_qt<T, HD, 1>(g, wide, static_cast<unsigned>(blocks), st);
   SPECA_HIP(hipGetLastError());

@@ -277,7 +277,7 @@ Args make_args(int dtype, const speca_kv_cache& c, const speca_kv_table& t, cons
 
 Error grid_of(const char* who, const Args& g, dim3* grid) {
   const int64_t blocks = packed_tiles(g.seqs, 1, PAGE, 1) * g.heads;
-  if (blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "%s: %d tokens of %d heads are too many for one call", who, g.seqs.total, g.heads);
+  if (blocks > kMaxBlocks) SPECA_FAIL(SPECA_EINVAL, "%s: %d tokens of %d heads are too many for one call", who, g.seqs.total, g.heads);
   *grid = dim3(static_cast<unsigned>(blocks), 2);
   return ok();
 }

@@ -6,6 +6,9 @@
 
 namespace speca {
 
+// Blocks of 256 threads that one launch may have: fewer than 2^32 threads along a dimension.
+constexpr int64_t kMaxBlocks = 0xFFFFFFFF / 256;
+
 Error launch_rope_axes(int dtype, const speca_rope& rope, const int32_t* positions, int64_t tokens, int head_dim, float eps,
                        const speca_rope_io& q, const speca_rope_io* k, hipStream_t st);
 

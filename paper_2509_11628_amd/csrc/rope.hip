@@ -301,7 +301,7 @@ Error launch_rope_axes(int dtype, const speca_rope& rope, const int32_t* positio
   g.steps_per_wave = (steps + g.chunks - 1) / g.chunks;
   g.chunks = (steps + g.steps_per_wave - 1) / g.steps_per_wave;
   const int64_t blocks = (tokens * g.chunks + 3) / 4;
-  if (blocks > 0x7FFFFFFF) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: %lld tokens are too many for one call", static_cast<long long>(tokens));
+  if (blocks > kMaxBlocks) SPECA_FAIL(SPECA_EINVAL, "speca_rope_axes: %lld tokens are too many for one call", static_cast<long long>(tokens));
   if (dtype == SPECA_BF16) launch_t<bf16_t>(g, vp, halves, static_cast<unsigned>(blocks), st);
   else launch_t<float>(g, vp, halves, static_cast<unsigned>(blocks), st);
   SPECA_HIP(hipGetLastError());

@@ -152,3 +152,17 @@ def test_how_few_rows_are_cut(tmp_path):
     assert r.returncode == 0, r.stderr
     r = subprocess.run([exe], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0 and "dealing is right" in r.stdout, r.stdout + r.stderr
+
+
+def test_more_blocks_than_a_launch_has_are_refused(bd):
+    """2^32 threads and more along one dimension are no launch: refused ahead of it, as the argument that it is."""
+    wide = 128 * 64
+    assert _rope(bd, tokens=1 << 26) == bd.EINVAL
+    for dtype in (0, 1):
+        assert _packed(bd, dtype=dtype, total=1 << 24, heads=128, kv=128, ldq=wide, ldk=wide, ldv=wide, ldo=wide) == bd.EINVAL
+    for name in ("speca_kv_store", "speca_kv_load"):
+        assert _code(bd, name, 1, _cache(bd, heads=128), bd.KVTable(A, 4), A, A, wide, A, wide, A, 2, 1 << 23) == bd.EINVAL
+    for n, total in ((2, 1 << 26), (1 << 21, 1 << 21), (1 << 20, 1 << 24)):
+        room = bd.load_library().speca_attention_cached_workspace(n, total, 20000, 64, 64, 64)
+        assert _code(bd, "speca_attention_cached", 1, A, 4096, A, 4096, A, n, total, _cache(bd, heads=64), bd.KVTable(A, 400), A, 20000, 64, 1, 0.0, A, room) == bd.EINVAL
+        assert "too many" in bd.load_library().speca_last_error(None).decode()
