@@ -260,12 +260,16 @@ def attention(qkv, heads: int, out=None):
 
 # ---- attention of packed and cached sequences ------------------------------------------------
 
+_INT_MAX = 2 ** 31 - 1          # sizes go to the library as int, and ctypes cuts off what does not fit
+
 
 def _heads(name, x, like=None):
     """A tensor [tokens, heads, head_dim] whose heads lie one after the other: its distance between tokens."""
     shape, stride = x.shape, x.stride()
     if len(shape) != 3 or (stride[2] != 1 and shape[2] > 1) or (stride[1] != shape[2] and shape[1] > 1):
         raise ValueError(f"{name}: [tokens, heads, head_dim] with the heads of a token in one piece is wanted, got {tuple(shape)} with strides {stride}")
+    if max(shape) > _INT_MAX:
+        raise ValueError(f"{name}: {tuple(shape)} is more than a call takes")
     if like is None:
         if not x.is_cuda or x.dtype not in _storage_types():
             raise ValueError(f"{name}: a bf16 or fp32 device tensor is wanted, got {x.dtype} on {x.device}")
@@ -291,7 +295,7 @@ def _ints(name, x, like, dims, rows=None, cols=None):
     import torch
     shape = x.shape
     if (x.dtype is not torch.int32 or x.get_device() != like.get_device() or len(shape) != dims or not x.is_contiguous()
-            or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols)):
+            or (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols) or max(shape) > _INT_MAX):
         want = [n if n is not None else "any" for n in (rows, cols)[:dims]]
         raise ValueError(f"{name}: contiguous int32 {want} on {like.device} is wanted, got {x.dtype} {tuple(shape)} on {x.device}")
     return x.data_ptr()
@@ -449,11 +453,12 @@ def attention_cached(q, starts, cache: KVCache, table, lens, causal: bool = True
     total, heads, hd = q.shape
     if not total:
         return out
-    longest = table.shape[1] * KV_PAGE if max_len is None else max_len
+    room = min(table.shape[1] * KV_PAGE, _INT_MAX)
+    longest = room if max_len is None else max(-1, min(max_len, room))
     size = load_library().speca_attention_cached_workspace(n, total, longest, heads, cache.desc.kv_heads, hd)
-    room = cache.k.new_empty(size) if size > 0 else None
+    work = cache.k.new_empty(size) if size > 0 else None
     _stand_alone(q, "speca_attention_cached", q.data_ptr(), ldq, out.data_ptr(), ldo, cu, n, total, cache.desc, t, at, longest, heads, int(causal), scale,
-                 None if room is None else room.data_ptr(), max(size, 0))
+                 None if work is None else work.data_ptr(), max(size, 0))
     return out
 
 

@@ -904,3 +904,15 @@ def test_captured_attention_over_lists_that_change(total):
         for s in range(n):
             if a[s + 1] > a[s] and b[s] == 0:
                 assert bool((out[a[s]:a[s + 1]] == 0).all())
+
+
+@pytest.mark.parametrize("max_len", [2 ** 31, 2 ** 32, 2 ** 32 + 70, 2 ** 40])
+def test_cached_bound_beyond_32_bits(max_len):
+    """A bound that no sequence reaches, however large: the bits without one."""
+    bd = _bd()
+    cache, table, _ = _fill(bd, [1500, 90], 2, 64)
+    q = ref.randn((4, 4, 64), torch.bfloat16, 1)
+    call = [q, ref.starts_of([3, 1]), cache, _dev(table), _dev([1500, 90])]
+    assert torch.equal(bd.attention_cached(*call, max_len=max_len), bd.attention_cached(*call))
+    with pytest.raises(bd.SpecaError):
+        bd.attention_cached(*call, max_len=-max_len)

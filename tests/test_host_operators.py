@@ -166,3 +166,17 @@ def test_more_blocks_than_a_launch_has_are_refused(bd):
         room = bd.load_library().speca_attention_cached_workspace(n, total, 20000, 64, 64, 64)
         assert _code(bd, "speca_attention_cached", 1, A, 4096, A, 4096, A, n, total, _cache(bd, heads=64), bd.KVTable(A, 400), A, 20000, 64, 1, 0.0, A, room) == bd.EINVAL
         assert "too many" in bd.load_library().speca_last_error(None).decode()
+
+
+def test_sizes_beyond_32_bits_are_refused_by_the_binding(bd):
+    """The library takes sizes as int: what does not fit is refused, not cut off."""
+    like = torch.empty((4, 2, 64), dtype=torch.bfloat16, device="meta")
+    for shape in ((2 ** 32 + 5, 2, 64), (2 ** 31, 2, 64), (4, 2 ** 32 + 2, 64)):
+        with pytest.raises(ValueError):
+            bd._heads("q", torch.empty(shape, dtype=torch.bfloat16, device="meta"), like)
+    for shape in ((2 ** 32 + 3,), (2 ** 31,)):
+        with pytest.raises(ValueError):
+            bd._ints("starts", torch.empty(shape, dtype=torch.int32, device="meta"), like, 1)
+    with pytest.raises(ValueError):
+        bd._ints("table", torch.empty((2, 2 ** 32 + 1), dtype=torch.int32, device="meta"), like, 2, 2)
+    assert bd._heads("q", torch.empty((2 ** 31 - 1, 2, 64), dtype=torch.bfloat16, device="meta"), like) == 128
