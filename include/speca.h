@@ -269,12 +269,13 @@ int speca_attention(void* hip_stream, int dtype, const void* qkv, void* out, int
 enum { SPECA_ROPE_ADJACENT = 0, SPECA_ROPE_HALVES = 1 };
 enum { SPECA_ROPE_PER_AXIS = 0, SPECA_ROPE_JOINT = 1 };
 #define SPECA_ROPE_MAX_AXES 4
-/* Rotary positions with several axes (time, height, width).  R = sum of dims features of a head turn in R / 2 pairs; the features
- * from R on stay.  Pair i is features (2i, 2i + 1) (ADJACENT) or (i, i + R / 2) (HALVES).  The first dims[0] / 2 pairs turn with
- * the first axis, the next dims[1] / 2 with the second, ...: pair j of axis a by
+/* Rotary positions with several axes (time, height, width).  R = sum of dims features of a head turn in R / 2 pairs; the
+ * features from R on stay (behind the norm, where there is one).  Pair i is features (2i, 2i + 1) (ADJACENT) or (i, i + R / 2)
+ * (HALVES).  The first dims[0] / 2 pairs turn with the first axis, the next dims[1] / 2 with the second, ...: pair j of axis a
+ * by
  *   position[a] * scale[a] * theta[a]^(-2 j / dims[a])        (PER_AXIS: every axis has its own spectrum)
  *   position[a] * scale[a] * theta[0]^(-2 i / R)              (JOINT: one spectrum over all pairs, i = pair of the head)
- * radians, formed in 64 bits, so far positions keep their angle. */
+ * radians, formed in 64 bits and rounded to 32 as a fraction of a turn, so far positions keep their angle to 10^-7. */
 typedef struct speca_rope {
   int32_t axes;                        /* 1 .. SPECA_ROPE_MAX_AXES */
   int32_t dims[SPECA_ROPE_MAX_AXES];   /* features of each axis: even, >= 2 */
@@ -300,7 +301,8 @@ int speca_rope_axes(void* hip_stream, int dtype, const speca_rope* rope, const i
  * scale 0 = 1 / sqrt(head_dim).  out: [total][heads][head_dim], tokens ldo apart; may not overlap the inputs.  head_dim 16, 32,
  * 64, 72 or 128.  What a token does not see has no part in its result, whatever it holds (infinities and NaN included).  bf16
  * runs on the bf16 matrix instructions where head_dim is 64, 72 or 128, q, k and v are 16-byte aligned with distances of whole 16
- * bytes (below 2^23 elements for k and v), out 8-byte; on the fp32 ones, five to ten times slower, elsewhere. */
+ * bytes (below 2^23 elements for k and v), out 8-byte; on the fp32 ones, five to ten times slower, elsewhere.  Scores, maxima and sums
+ * are fp32; the bf16 instructions take the probabilities in bf16 (as speca_attention does), which adds at most 2^-8 of sum p |v|. */
 int speca_attention_packed(void* hip_stream, int dtype, const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv,
                            void* out, int64_t ldo, const int32_t* starts, int n_seqs, int total, int heads, int kv_heads, int head_dim,
                            int causal, float scale);
@@ -310,11 +312,12 @@ int speca_attention_packed(void* hip_stream, int dtype, const void* q, int64_t l
  *   v        bytes [pages][kv_heads][head_dim][64 tokens], token 16 m + 4 g + i of the page at place 16 g + 4 m + i (m, g, i < 4):
  *            what one lane of a matrix instruction reads is then 16 bytes in one piece
  *   k_scale, v_scale  float [pages][kv_heads]
- * A byte is e4m3 (OCP: largest 448, 0x7F and 0xFF are NaN) and stands for its value x the scale of its page and head, a power of
- * two 2^e with -100 <= e <= 119, the smallest whose 448-fold reaches every finite value that was stored in the page (or larger,
- * where larger tokens have been overwritten).  With powers of two, bytes times scale are exact in bf16, and a page that grows
- * keeps its tokens' values when a larger token takes the scale up, unless they become subnormal (below scale / 64; then rounded
- * once more). k and v must be 16-byte aligned.  head_dim 16, 32, 64, 72 or 128. */
+ * A byte is e4m3 (OCP: largest 448, 0x7F and 0xFF are NaN) and stands for its value x the scale of its page and head, a power
+ * of two 2^e with -100 <= e <= 119, the smallest whose 448-fold reaches every finite value that was stored in the page (or
+ * larger, where larger tokens have been overwritten; 448 x 2^119 is the largest value held).  With powers of two, bytes times
+ * scale are exact in bf16, and a page that grows keeps its tokens' values when a larger token takes the scale up, unless they
+ * become subnormal (below scale / 64; then rounded once more). k and v must be 16-byte aligned.  head_dim 16, 32, 64, 72 or
+ * 128. */
 #define SPECA_KV_PAGE 64
 typedef struct speca_kv_cache {
   void* k;
@@ -330,9 +333,11 @@ typedef struct speca_kv_table {
   int32_t ld;
 } speca_kv_table;
 
-/* Tokens of the packed k and v ([total][kv_heads][head_dim] of type dtype) become tokens past[s], past[s] + 1, ... of sequence s (past: DEVICE
- * int32 [n_seqs], >= 0).  Rounding to nearest, ties to even; infinities saturate, NaN stays.  Tokens of a page below past[s] are
- * kept, what lay from the last new token on in its page is cleared.  Two sequences of one call must not write the same page. */
+/* Tokens of the packed k and v ([total][kv_heads][head_dim] of type dtype) become tokens past[s], past[s] + 1, ... of sequence
+ * s (past: DEVICE int32 [n_seqs], >= 0).  Rounding to nearest, ties to even; infinities, and values beyond 448 x 2^119, become
+ * 448 x the page's scale, NaN stays.  Tokens of a page below past[s] are kept, what lay behind the last new token in its page
+ * is cleared.  One call must not write a page twice, neither for two sequences nor for two places of one (the results would be
+ * those of either or a mixture). */
 int speca_kv_store(void* hip_stream, int dtype, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* past,
                    const void* k, int64_t ldk, const void* v, int64_t ldv, const int32_t* starts, int n_seqs, int total);
 /* The other way round: tokens first[s], first[s] + 1, ... of sequence s, as the values they stand for, into packed k and v.  (In both calls a run
@@ -342,11 +347,12 @@ int speca_kv_load(void* hip_stream, int dtype, const speca_kv_cache* cache, cons
 
 /* Attention of the new tokens q ([total][heads][head_dim], bf16) over the first lens[s] tokens of their sequence in the cache
  * (lens: DEVICE int32 [n_seqs]; the new tokens' own keys are among them if they were stored).  causal != 0: of n new tokens the
- * i-th sees tokens 0 .. lens[s] - n + i. A token that sees nothing (lens[s] = 0, or causal with more new tokens than held) gives
- * 0.  max_len: no sequence is longer (tokens from there on are not attended to); it sets how the work is split, as n_seqs and
- * total do.  out: bf16, tokens ldo apart; may not overlap q. dtype: SPECA_BF16 (SPECA_F32 is SPECA_EUNSUPPORTED).  workspace:
- * DEVICE, 16-byte aligned, of at least speca_attention_cached_workspace bytes, in use until the call's work has ended; calls that
- * may overlap need one each. */
+ * i-th (from 0) sees tokens 0 .. lens[s] - n + i. A token that sees nothing (lens[s] = 0, or causal with more new tokens than
+ * held) gives 0.  max_len (0 .. 2^30): no sequence is longer (tokens from there on are not attended to; where the new ones stand
+ * follows from lens[s] as it is); it sets how the work is split, as n_seqs and total do.  Scores, maxima and sums are fp32, the
+ * probabilities bf16 for the matrix instructions, which adds at most 2^-8 of sum p |v|.  out: bf16, tokens ldo apart; may not
+ * overlap q.  dtype: SPECA_BF16 (SPECA_F32 is SPECA_EUNSUPPORTED).  workspace: DEVICE, 16-byte aligned, of at least
+ * speca_attention_cached_workspace bytes, in use until the call's work has ended; calls that may overlap need one each. */
 int speca_attention_cached(void* hip_stream, int dtype, const void* q, int64_t ldq, void* out, int64_t ldo, const int32_t* starts, int n_seqs,
                            int total, const speca_kv_cache* cache, const speca_kv_table* table, const int32_t* lens, int max_len, int heads,
                            int causal, float scale, void* workspace, int64_t workspace_bytes);

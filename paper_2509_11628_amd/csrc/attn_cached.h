@@ -176,8 +176,11 @@ __device__ inline int keys_of(const CachedArgs& g, int held, int len, int n, int
 // of them ends sooner (few tiles: 256 tokens over 4096 and over 1024, 16 heads of 72: 43 us), and where no sequence is longer than
 // kLeastPages pages: then nothing is split, and a block takes every so many.
 // With whole rounds of even splits instead of borders (us): a frame of 1590 tokens over 27 286, 24 heads of 128, 648 instead of 618; a prompt of
-// 4096 tokens over itself, causal, 32 heads over 8, 286 instead of 174; 512 tokens over 8192 124 instead of 106.  A tile's cost of 6 or 9
-// positions instead of 4: 0.2 and 1.2 % slower over 37 batches.
+// 4096 tokens over itself, causal, 32 heads over 8 of 128, 286 instead of 174; 512 tokens over 8192, the same heads, 124 instead of 106.  A tile's
+// cost of 6 or 9 positions instead of 4 is no faster.
+//   Causal tiles count with all pages of their sequence, though the early ones of a prompt see few: what they do not see is skipped, and a block
+// whose part it was is done early.  Where a part is shorter than two tiles that leaves much of the chip without work (3000 tokens over themselves, 12
+// heads of 128, 114 us; 2000, 24 heads, 106; 4096, 32 heads over 8, two tiles a part, 175; the packed kernel takes 65, 48 and 149).
 constexpr int kTileCost = 4, kLeastPart = 8, kLeastPages = 16;
 // Causal tiles see the more pages the later they are: the first, the last, the second, ... so that neighbours have the same work together.
 __device__ inline int tile_in_line(int j, int tiles, bool causal) { return !causal ? j : j & 1 ? tiles - 1 - (j >> 1) : j >> 1; }

@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256, 2) void attention_cached_kernel(const CachedAr
               if (hit[i][e] > 0.0f) o[dt][i][e] = __uint_as_float(0x7FC00000u);
         }
       }
-      bf16x8 pf[2][NQ];
+      bf16x8 pf[2][NQ];                              // rounded to bf16 for the matrix instructions; their sum, in fp32, has them unrounded
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -479,7 +479,10 @@ Plan plan_of(int n_seqs, int total, int max_len, int heads, int kv_heads, int he
   p.resident = 2 * compute_units();
   // Fewer pages a unit spread a call over more blocks; what begins, ends and joins one costs as much as a few pages.  Few rows: 8 (33 tokens
   // of 13 sequences of up to 9756, 28 heads over 4: 20.9 us, 22.1 with 6, 23.9 with 4, 27.5 with 24), but no splits at all, and no second
-  // launch, up to 20 pages (four sequences of up to 1200: 13.8 us, 18.2 with splits of 6).
+  // launch, where no sequence can have more than 20 pages.  One token each, 32 heads over 8 of 128, us uncut / in splits of 8: one sequence of 16
+  // pages 11.4 / 14.9, of 20 12.4 / 15.0, 21 13.0 / 15.2, 24 13.6 / 15.3, 32 16.3 / 14.9, 64 26.7 / 15.3; four of 20 13.4 / 15.0, 24 14.9 / 15.0, 32
+  // 17.3 / 15.2, 128 48.9 / 21.7; sixteen, which fill half the chip, 20 14.7 / 18.8, 64 29.1 / 31.8, 128 50.7 / 51.7.  (The bound is max_len's, for
+  // the host knows no lengths: a bound far above them costs the second launch, 11 to 15 us for short ones.)
   p.least_pages = p.rows == 128 ? kLeastPages : pages <= 20 ? 20 : 8;
   const int64_t whole = p.tiles * kv_heads;
   if (pages > p.least_pages) {

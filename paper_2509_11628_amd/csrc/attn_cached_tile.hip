@@ -10,8 +10,8 @@
 // page stores them: 16 bytes are one dimension's keys of one lane group, in the order in which S^T hands them on.  Their two widened halves
 // go to place [half][tile of 16 dimensions][lane], so a fragment is one read of 16 bytes per lane, all lanes in a row.
 //
-// What bounds it: the vector unit (exponentials, maxima, widening) and the LDS reads beside the matrix instructions, at two blocks per
-// unit.  A frame of 1590 tokens over 27 286, 24 heads of 128: 615 to 630 us with the join, 845 to 865 TFLOP/s.  On the way there, us:
+// What bounds it: the vector unit (exponentials, maxima, widening; 55 % busy, the matrix unit 39 %, LDS 12 %) and what waves wait for, at two
+// blocks per unit.  A frame of 1590 tokens over 27 286, 24 heads of 128: 615 to 630 us with the join, 845 to 865 TFLOP/s.  On the way there, us:
 // widening in every wave's registers instead (rows of 64 a wave) 1150; through LDS 950; without bank conflicts of the writes 745 with those
 // of the values, 683 with those of the keys gone; without registers that spill to memory, whose restores wait for the bytes on their way, 647
 // (three or four fragments ahead instead of two spill again: 650 and 715; keys in units of 8 bytes, which spares the turn below, 802).
@@ -392,7 +392,8 @@ __global__ __launch_bounds__(256, 2) void attention_cached_tile_kernel(const Cac
           psum[e] += p;
         }
       };
-      auto pack = [&](const floatx4 (&s)[4][2], int u, int i) {        // P^T of keys 32 u .. 32 u + 31
+      // P^T of keys 32 u .. 32 u + 31, rounded to bf16 for the matrix instructions; the sum, in fp32, has them unrounded
+      auto pack = [&](const floatx4 (&s)[4][2], int u, int i) {
         Frag x;
         x.q = make_uint4(cvt_pk_bf16(s[2 * u][i][0], s[2 * u][i][1]), cvt_pk_bf16(s[2 * u][i][2], s[2 * u][i][3]),
                          cvt_pk_bf16(s[2 * u + 1][i][0], s[2 * u + 1][i][1]), cvt_pk_bf16(s[2 * u + 1][i][2], s[2 * u + 1][i][3]));

@@ -72,7 +72,8 @@ __device__ inline void vt_write_off(int d, int kb, int* lo, int* hi) {
 //         32 u + 16 + 4 g for group g two such reads are one A fragment of V^T in exactly the key order in which the S^T
 //         accumulators hand P^T on.  Two groups read 8 rows x 32 bytes at a time: chunk c of row r sits at position
 //         c ^ (2 (r & 7)) (head_dim 128) or c ^ (2 ((r >> 1) & 3)) (64).
-// head_dim 72: rows of 144 bytes spread over the banks by themselves.  Its last score step covers columns 64 .. 95: beyond 71
+// head_dim 72: rows of 144 bytes are not permuted; they spread over the banks, but not evenly (41 % of the LDS cycles of short packed sequences
+// are conflicts).  Its last score step covers columns 64 .. 95: beyond 71
 // the lanes read zeros (not the next row: it may hold infinities), and value dims 72 .. 79 repeat a chunk, for results that are
 // never stored.
 // Keys and values beyond T read as zeros (the buffer ends there); their scores are masked to -inf, and the probability 0 meets no
@@ -115,10 +116,13 @@ __device__ __forceinline__ void buffer_to_lds(const uint16_t* buffer, int bytes,
 }
 
 // Rows of equal length (PLAIN), or packed sequences, of which causal tokens see themselves and those before them.
-// Packed, one MI355X: 5 sequences of 589 to 4608 tokens, 24 heads of 128: 605 to 640 us, 950 to 1010 TFLOP/s (power, as above); 12 causal
-// ones of 19 to 4096, 32 heads over 8 of 128: 334 to 345 us, 820 to 845 TFLOP/s of the products that count (a block's last two tiles are
-// half hidden); 16 of 1 to 400 tokens, 16 heads of 72: 17.5 us, a chain of waits (places, first tiles, up to 7 tiles), in which the keys of
+// Packed, one MI355X: 5 sequences of 589 to 4608 tokens, 24 heads of 128: 605 to 640 us, 950 to 1010 TFLOP/s (power, as above; vector unit 60 %
+// busy, matrix unit 48 %); 12 causal ones of 19 to 4096, 32 heads over 8 of 128: 314 to 330 us, 855 to 900 TFLOP/s of the products that count
+// (61 and 41 %); 16 of 1 to 400 tokens, 16 heads of 72: 17.5 us, a chain of waits (places, first tiles, up to 7 tiles), in which the keys of
 // several heads a cache line go to one XCD.
+// The mask costs 11 % at these lengths (TFLOP/s without it and with it: the 12 sequences 1010 and 898, one of 4096 1037 and 915, one of 16 384 1108
+// and 1077): what a block takes to begin and end, about four tiles' time, falls on half as many tiles, and two waves only load the last one.
+// Neither the order of the sequences (sorted by length 900) nor their being ragged (eight of 2048 833) is what is lost.
 enum { PLAIN = 0, PACKED = 1, CAUSAL = 2 };
 struct TileArgs {
   const uint16_t *q, *k, *v;
@@ -288,7 +292,8 @@ __global__ __launch_bounds__(256, 2) void attention_dma_kernel(const TileArgs g)
       psum[n] += p;
     }
   };
-  auto pack = [&](const floatx4 (&s)[4][2], int u, int n) {        // P^T of keys 32 u .. 32 u + 31
+  // P^T of keys 32 u .. 32 u + 31, rounded to bf16 for the matrix instructions, half a step (2^-8 of a value) each; the sum, in fp32, has them unrounded
+  auto pack = [&](const floatx4 (&s)[4][2], int u, int n) {
     Frag pf;
     pf.u = make_uint4(cvt_pk_bf16(s[2 * u][n][0], s[2 * u][n][1]), cvt_pk_bf16(s[2 * u][n][2], s[2 * u][n][3]),
                       cvt_pk_bf16(s[2 * u + 1][n][0], s[2 * u + 1][n][1]), cvt_pk_bf16(s[2 * u + 1][n][2], s[2 * u + 1][n][3]));

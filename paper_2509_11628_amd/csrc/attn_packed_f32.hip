@@ -6,8 +6,10 @@
 // O^T in pieces of four (tile i % 4 of group i / 4 owns dimensions 64 g + 4 row + i), so a lane's values are 16-byte pieces of V and of the
 // output. T = storage type of q, k, v and the output; arithmetic is fp32.
 //
-// What bounds it: fragments straight from memory (16 rows x 64 bytes per load), of which a unit takes 33 to 34 bytes per ns.  Sequences of
-// 1024, 77, 777 and 256 tokens, 6 heads of 64: 38 us, 69 TFLOP/s; with 32 queries a block 44, for want of blocks.
+// What bounds it: issue, not memory.  Sequences of 1024, 77, 777 and 256 tokens, 6 heads of 64: 38 us, 69 TFLOP/s.  The matrix unit is busy
+// for 54 % of a block's life and the vector unit for 36 %; waves spend 65 % of theirs waiting for their turn at them and 18 % for data; with
+// every key and value from a wave's first four tiles, which then lie in its cache, the time is the same.  The 804 blocks leave some units
+// four where others have three.  The exponential is the hardware's instruction alone, off by about a unit in the last place.
 #include "attn_lane.h"
 #include "operators.h"
 
@@ -276,7 +278,10 @@ Error launch_hd(const Args& g, hipStream_t st) {
   const PackedAttention& a = g.a;
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.out);
   const bool wide = at % (4 * sizeof(T)) == 0 && (a.ldq | a.ldk | a.ldv | a.ldo) % 4 == 0;
-  // 32 queries per block read every key and value half as often; 16 keep the chip busy when there are few of them (above: 396 blocks of 32)
+  // 32 queries per block read every key and value half as often; 16 keep the chip busy when there are few blocks, and waste less where sequences or
+  // what causal queries see end.  us, 32 / 16: up to 512 blocks 16 are never slower (396 blocks, the sequences above, 47 / 42; 192 blocks 104 / 86);
+  // beyond, without mask, 16 heads of 72 over 4096 tokens 858 / 1059, 8 of 16 124 / 140, 24 of 128 2081 / 2128, 4 x 1024 tokens of 6 heads of 64
+  // 75 / 72, 20 x 300 of 24 of 128 374 / 307; causal, 16 heads of 72 over 4096 588 / 676, 24 of 128 1413 / 1230, 6 of 64 217 / 164.
   const bool two = static_cast<int64_t>(a.seqs.total / 32) * a.heads >= 512;
   const int64_t blocks = packed_tiles(a.seqs, 1, two ? 32 : 16, 0) * a.heads;
   if (blocks > kMaxBlocks) SPECA_FAIL(SPECA_EINVAL, "speca_attention_packed: %d tokens of %d heads are too many for one call", a.seqs.total, a.heads);

@@ -5,8 +5,8 @@
 //
 // A page and head is one block's, for keys and for values each: amax needs all of its new tokens, and the bytes that stay need the old scale.
 // Bound by memory and by the chain of waits of one block (place, tokens, maximum, bytes).  Storing 2512 tokens of 24 heads of 128 in bf16
-// takes 16 us, loading them back 12 (45 MB each way); 16 single tokens of 8 heads 6 and 4.  One value per thread at a time took 51 and 30,
-// 14 and 12.
+// takes 15 us, loading them back 11 (46 MB each way); 16 single tokens of 8 heads 6 and 4.  One value per thread at a time took 51 and 30,
+// 14 and 12.  In fp32 17 and 46 us (78 MB each way; a row's two halves of 16 bytes go out one after the other), 6 and 7.
 #include "operators.h"
 
 namespace speca {

@@ -916,3 +916,12 @@ def test_cached_bound_beyond_32_bits(max_len):
     assert torch.equal(bd.attention_cached(*call, max_len=max_len), bd.attention_cached(*call))
     with pytest.raises(bd.SpecaError):
         bd.attention_cached(*call, max_len=-max_len)
+
+
+@pytest.mark.parametrize("hd", [64, 72])
+@pytest.mark.parametrize("H,Hkv", [(8, 8), (16, 16), (24, 24), (16, 8), (48, 16)])
+def test_packed_key_heads_by_the_eight(hd, H, Hkv):
+    """As many key heads as there are XCDs, and multiples: every head gets its own keys however heads are dealt."""
+    bd = _bd()
+    for causal in (False, True):
+        _packed_check(bd, [130, 3, 77], H, Hkv, hd, "bf16", causal, seed=3)
